@@ -406,6 +406,26 @@ int32_t precc_combine_partials(precc_ctx* ctx, const precc_layer_desc* desc, con
                                int32_t n_shards, int32_t B, const int32_t* agent_id, const void* B_v,
                                void* out, void* stream);
 
+/* ---------------------------------------------------------------- around the cached attention
+ * The norm that makes the hidden states H, and the query / output projections of a batch whose rows belong to different
+ * agents.  Like every call they are asynchronous and capturable.  They are programmatic dependent launches that
+ * read and write nothing before the kernel ahead of them on the stream has completed. */
+
+/* Root-mean-square norm with the residual's addition, row by row, in fp32:
+ *   s = x + residual,  residual_out = bf16(s),  y = s / sqrt(mean(s^2) + eps) * gain
+ *   out = bf16(y);  out_scale = max |y| / 448 of the row, out_e4m3 = e4m3(y / out_scale)
+ *   x, residual, residual_out, out  [rows][width]; residual NULL: s = x; residual_out NULL: not written; out may be NULL when
+ *                 out_e4m3 is given
+ *   gain          [width]
+ *   out_e4m3      [rows][width] e4m3 and out_scale, device fp32 [rows], go together; both NULL: no 8-bit output.  The
+ *                 scale of a row of zeros is 1; scales are not smaller than the least normal fp32.
+ * Outputs may be x or residual themselves (the same address); other overlaps are not allowed.  A row with a NaN or an infinity is NaN
+ * in that place of `out` or in all of it, has a NaN or infinite scale, and touches no other row.  The norm is of
+ * the unrounded sum.  width: a multiple of 8, at most 32768.  rows == 0 is a no-op. */
+int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, const void* gain, int32_t rows,
+                       int32_t width, float eps, void* residual_out, void* out, void* out_e4m3,
+                       float* out_scale, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,6 +29,7 @@ EXPORTS = [
     "precc_set_wait_limit", "precc_selftest_wait_timeout",
     "precc_prefill_rope_scratch_bytes", "precc_lr_attend_prefill_rope_scratch",
     "precc_prefill_ws_bytes", "precc_lr_attend_prefill_ws",
+    "precc_rms_norm",
 ]
 
 
@@ -117,6 +118,7 @@ def load_library() -> C.CDLL:
     lib.precc_lr_attend_decode_partial.argtypes = [vp, C.POINTER(LayerDesc), vp, i32, vp, vp, vp, i32, vp, i32, vp,
                                                    C.POINTER(CacheDesc), vp, vp, sz, vp]
     lib.precc_combine_partials.argtypes = [vp, C.POINTER(LayerDesc), vp, i32, i32, vp, vp, vp, vp]
+    lib.precc_rms_norm.argtypes = [vp, vp, vp, vp, i32, i32, C.c_float, vp, vp, vp, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int:  # default restype: the int32 status code
@@ -364,3 +366,11 @@ class Precc:
         """Prefill with a caller-provided workspace (uint8 tensor of prefill_ws_bytes, or None): helper blocks on idle SMs."""
         _native.lr_attend_prefill_ws(self._ctx, desc, q, agent, ctx_len, B_k, B_v, cache, out, workspace, block_table,
                                      first_block)
+
+    # ------------------------------------------------------------------ around the cached attention
+    def rms_norm(self, x: torch.Tensor, gain: torch.Tensor, eps: float, out: Optional[torch.Tensor] = None,
+                 residual: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None,
+                 out_e4m3: Optional[torch.Tensor] = None, out_scale: Optional[torch.Tensor] = None):
+        """Norm of x (+ residual) over its last dimension: bf16 into ``out``, 8 bits with one fp32 scale per row into ``out_e4m3`` /
+        ``out_scale``, the sum itself into ``residual_out`` (which may be ``residual``)."""
+        _native.rms_norm(self._ctx, x, gain, eps, out, residual, residual_out, out_e4m3, out_scale)

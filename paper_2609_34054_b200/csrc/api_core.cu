@@ -66,6 +66,13 @@ int32_t check_cache(precc_ctx* ctx, const precc_layer_desc* d, const precc_cache
   return PRECC_OK;
 }
 
+int32_t check_device(precc_ctx* ctx) {
+  int cur = -1;
+  PRECC_CUDA(ctx, cudaGetDevice(&cur));
+  if (cur != ctx->device) return fail(ctx, PRECC_ERR_INVALID_ARG, "current device %d is not the context's device %d", cur, ctx->device);
+  return PRECC_OK;
+}
+
 float softmax_scale_log2(const precc_layer_desc* d) {
   const float sc = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / std::sqrt((float)d->head_dim);
   return sc * 1.4426950408889634f;

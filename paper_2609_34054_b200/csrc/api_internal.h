@@ -79,6 +79,7 @@ std::recursive_mutex& lazy_mu();
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool rank_ok(int r) { return r == 8 || r == 16 || r == 32 || r == 64; }
 int32_t check_desc(precc_ctx* ctx, const precc_layer_desc* d);
+int32_t check_device(precc_ctx* ctx);        // the context's device is the current one
 int32_t check_cache(precc_ctx* ctx, const precc_layer_desc* d, const precc_cache* c, bool need_base, bool need_lr);
 float softmax_scale_log2(const precc_layer_desc* d);
 

@@ -1,0 +1,56 @@
+// libprecc: the norm of hidden states ahead of the projections.
+#include "api_internal.h"
+#include "norm.cuh"
+
+using namespace precc;
+
+namespace {
+
+template <int C, bool SHORT>
+int32_t norm_launch(precc_ctx* ctx, const NormParams& p, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  const int rows_per_block = SHORT ? NORM_SHORT_THREADS / p.T : 1;
+  cfg.gridDim = dim3((unsigned)((p.rows + rows_per_block - 1LL) / rows_per_block));
+  cfg.blockDim = dim3(SHORT ? NORM_SHORT_THREADS : p.T);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  PRECC_CUDA(ctx, cudaLaunchKernelEx(&cfg, rms_norm_kernel<C, SHORT>, p));
+  return PRECC_OK;
+}
+
+}  // namespace
+
+extern "C" int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, const void* gain, int32_t rows,
+                                  int32_t width, float eps, void* residual_out, void* out, void* out_e4m3, float* out_scale,
+                                  void* stream) {
+  if (!ctx) return PRECC_ERR_INVALID_ARG;
+  if (rows < 0 || width <= 0) return fail(ctx, PRECC_ERR_INVALID_ARG, "rows < 0 or width <= 0");
+  if (width % 8 || width > NORM_MAX_WIDTH) return fail(ctx, PRECC_ERR_UNSUPPORTED, "width %d not a multiple of 8 up to %d", width, NORM_MAX_WIDTH);
+  if (!(eps >= 0.f)) return fail(ctx, PRECC_ERR_INVALID_ARG, "eps is negative or NaN");
+  if (rows == 0) return PRECC_OK;
+  if (!x || !gain) return fail(ctx, PRECC_ERR_INVALID_ARG, "x / gain is null");
+  if (!out && !out_e4m3) return fail(ctx, PRECC_ERR_INVALID_ARG, "neither a bf16 nor an 8-bit output is given");
+  if ((out_e4m3 != nullptr) != (out_scale != nullptr)) return fail(ctx, PRECC_ERR_INVALID_ARG, "the 8-bit output and its scales come together");
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(residual_out) || !aligned16(out) || !aligned16(out_e4m3) ||
+      (reinterpret_cast<uintptr_t>(out_scale) & 3u))
+    return fail(ctx, PRECC_ERR_MISALIGNED, "x / residual / gain / residual_out / out / out_e4m3 not 16-byte aligned (out_scale: 4)");
+  const int32_t rc = check_device(ctx);
+  if (rc) return rc;
+  NormParams p;
+  p.x = (const __nv_bfloat16*)x; p.residual = (const __nv_bfloat16*)residual; p.gain = (const __nv_bfloat16*)gain;
+  p.residual_out = (__nv_bfloat16*)residual_out; p.out = (__nv_bfloat16*)out; p.q = (uint8_t*)out_e4m3; p.q_scale = out_scale;
+  p.rows = rows; p.pieces = width / 8; p.inv_width = 1.0f / width; p.eps = eps;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (p.pieces <= 32) {
+    p.T = 1;
+    while (p.T < p.pieces) p.T *= 2;
+    return norm_launch<1, true>(ctx, p, st);
+  }
+  auto threads = [&](int c) { return ((p.pieces + c - 1) / c + 31) / 32 * 32; };
+  if (threads(1) <= 1024) { p.T = threads(1); return norm_launch<1, false>(ctx, p, st); }
+  p.T = threads(4);
+  return norm_launch<4, false>(ctx, p, st);
+}

@@ -1,0 +1,130 @@
+// Root-mean-square norm of hidden states with the residual's addition, bf16 and / or 8-bit output:
+//   s = x + residual,  residual_out = bf16(s),  y = s / sqrt(mean(s^2) + eps) * gain
+//   bf16 output: bf16(y);  8-bit output: scale = max |y| / 448 of the row (1 for a row of zeros), q = e4m3(y / scale)
+//
+// HBM-bound: a row is read once, kept in registers as fp32 from the addition to the last rounding (the norm is of the unrounded
+// sum; every output is rounded once), and written once.  A thread holds C pieces of eight columns, piece i of the row at thread
+// i % T, so that a warp's loads are 512 consecutive bytes.
+#pragma once
+#include "common.cuh"
+
+namespace precc {
+
+constexpr int NORM_MAX_WIDTH = 32768;
+constexpr int NORM_SHORT_THREADS = 128;      // block of rows that fit a warp or a part of one
+constexpr float E4M3_MAX = 448.f;
+
+struct NormParams {
+  const __nv_bfloat16* x;
+  const __nv_bfloat16* residual;             // or null
+  const __nv_bfloat16* gain;
+  __nv_bfloat16* residual_out;               // or null
+  __nv_bfloat16* out;                        // or null
+  uint8_t* q;                                // or null
+  float* q_scale;
+  int rows, pieces;                          // pieces of eight columns in a row
+  int T;                                     // threads of a row
+  float inv_width, eps;
+};
+
+// max that lets a NaN through (fmaxf drops it): a row with a NaN gets a NaN scale, not a plausible one
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(lo) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(hi) : "f"(d), "f"(c));
+  return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
+}
+__device__ __forceinline__ void unpack_bf16x8(const uint4& v, float (&f)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ uint4 pack_bf16x8(const float (&f)[8]) {
+  return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// C pieces per thread.  SHORT: several rows of T <= 32 threads (a power of two) in a block of NORM_SHORT_THREADS; else one row
+// of blockDim.x = T threads.
+template <int C, bool SHORT>
+__global__ void __launch_bounds__(SHORT ? NORM_SHORT_THREADS : 1024)
+rms_norm_kernel(const NormParams p) {
+  __shared__ float part[2][32];
+  const int t = SHORT ? threadIdx.x % p.T : threadIdx.x;
+  const long long row = SHORT ? (long long)blockIdx.x * (NORM_SHORT_THREADS / p.T) + threadIdx.x / p.T : blockIdx.x;
+  const bool live = !SHORT || row < p.rows;
+  // over the threads of a row; every thread gets the result
+  auto reduce = [&](float v, int slot, auto op) {
+    for (int m = (SHORT ? p.T : 32) / 2; m > 0; m >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, m));
+    if constexpr (!SHORT) {
+      const int warps = p.T / 32;
+      if ((threadIdx.x & 31) == 0) part[slot][threadIdx.x / 32] = v;
+      __syncthreads();
+      v = part[slot][0];
+      for (int w = 1; w < warps; ++w) v = op(v, part[slot][w]);
+    }
+    return v;
+  };
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long at = row * p.pieces;       // in pieces of eight columns
+  float s[C][8];
+  float sum = 0.f;
+  uint4 xv[C], rv[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int i = t + c * p.T;
+    xv[c] = rv[c] = make_uint4(0, 0, 0, 0);
+    if (live && i < p.pieces) {
+      xv[c] = reinterpret_cast<const uint4*>(p.x)[at + i];
+      if (p.residual) rv[c] = reinterpret_cast<const uint4*>(p.residual)[at + i];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    float r[8];
+    unpack_bf16x8(xv[c], s[c]);
+    unpack_bf16x8(rv[c], r);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { s[c][k] += r[k]; sum = fmaf(s[c][k], s[c][k], sum); }
+  }
+  if (p.residual_out) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int i = t + c * p.T;
+      if (live && i < p.pieces) reinterpret_cast<uint4*>(p.residual_out)[at + i] = pack_bf16x8(s[c]);
+    }
+  }
+  sum = reduce(sum, 0, [](float a, float b) { return a + b; });
+  const float inv = 1.0f / sqrtf(fmaf(sum, p.inv_width, p.eps));
+  float top = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int i = t + c * p.T;
+    if (live && i < p.pieces) {
+      float g[8];
+      unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(p.gain) + i), g);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) { s[c][k] = s[c][k] * inv * g[k]; top = max_nan(top, fabsf(s[c][k])); }
+      if (p.out) reinterpret_cast<uint4*>(p.out)[at + i] = pack_bf16x8(s[c]);
+    }
+  }
+  if (!p.q) return;
+  top = reduce(top, 1, [](float a, float b) { return max_nan(a, b); });
+  const float scale = top == 0.f ? 1.f : max_nan(top * (1.f / E4M3_MAX), 1.17549435e-38f);     // (a normal number, and so is its reciprocal)
+  const float to_q = 1.0f / scale;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int i = t + c * p.T;
+    if (live && i < p.pieces)
+      reinterpret_cast<uint2*>(p.q)[at + i] = make_uint2(pack_e4m3x4(s[c][0] * to_q, s[c][1] * to_q, s[c][2] * to_q, s[c][3] * to_q),
+                                                         pack_e4m3x4(s[c][4] * to_q, s[c][5] * to_q, s[c][6] * to_q, s[c][7] * to_q));
+  }
+  if (live && t == 0) p.q_scale[row] = scale;
+}
+
+}  // namespace precc

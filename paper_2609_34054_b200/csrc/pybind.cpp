@@ -10,6 +10,7 @@
 // frames: every entry point runs inside `guarded`, dimensions are checked before a size is read, and pointers and sizes
 // are taken while the GIL is held.
 #include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -27,6 +28,7 @@ PyObject *s_desc, *s_k_base, *s_v_base, *s_lr_k, *s_lr_v, *s_n_blocks;
 struct Args {
   PyObject* const* at;
   bool ok;
+  int device = -1;         // of the tensors looked at by check()
   Args(PyObject* const* a, Py_ssize_t n, Py_ssize_t want) : at(a), ok(n == want) {
     if (!ok) PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, n);
   }
@@ -74,6 +76,46 @@ struct Args {
     const at::Tensor* t = required(name);
     if (t && t->dim() < 1) { PyErr_Format(g_error, "%s has no dimensions", name); ok = false; }
     return ok ? Rows{t->data_ptr(), static_cast<int32_t>(t->size(0))} : Rows{nullptr, 0};
+  }
+  // A tensor of a given type and number of elements (None where `required` is false).  The calls around the attention take their
+  // sizes from the tensors, so that no size can disagree with a buffer, and want them all on one device, the current one.
+  void* sized(const char* name, c10::ScalarType type, int64_t n, bool required) {
+    const at::Tensor* t = tensor();
+    if (!ok) return nullptr;
+    if (!t) {
+      if (required) { PyErr_Format(g_error, "%s is None", name); ok = false; }
+      return nullptr;
+    }
+    check(name, *t, type);
+    if (ok && t->numel() != n) { PyErr_Format(g_error, "%s has %lld elements, expected %lld", name, (long long)t->numel(), (long long)n); ok = false; }
+    return ok ? t->data_ptr() : nullptr;
+  }
+  void check(const char* name, const at::Tensor& t, c10::ScalarType type) {
+    if (t.scalar_type() != type) { PyErr_Format(g_error, "%s must be %s", name, c10::toString(type)); ok = false; }
+    else if (device < 0) device = t.get_device();
+    else if (t.get_device() != device) { PyErr_Format(g_error, "%s is on another device than the tensors before it", name); ok = false; }
+  }
+  bool on_current_device() {
+    if (ok && device >= 0 && device != c10::cuda::current_device()) bad("the tensors are not on the current device");
+    return ok;
+  }
+  // A required tensor [..., width]: address, number of rows, width.
+  struct Matrix { void* p; int64_t rows, width; };
+  Matrix matrix(const char* name, c10::ScalarType type) {
+    const at::Tensor* t = required(name);
+    if (ok && t->dim() < 1) { PyErr_Format(g_error, "%s has no dimensions", name); ok = false; }
+    if (ok) check(name, *t, type);
+    if (!ok) return {nullptr, 0, 0};
+    const int64_t w = t->size(t->dim() - 1), rows = w > 0 ? t->numel() / w : 0;
+    if (rows > INT32_MAX || w > INT32_MAX) { bad("a matrix of this call has more than 2^31 - 1 rows or columns"); return {nullptr, 0, 0}; }
+    return {t->data_ptr(), rows, w};
+  }
+  float f32() {
+    PyObject* o = next();
+    if (!ok) return 0.f;
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) ok = false;
+    return static_cast<float>(v);
   }
   // Block table or None: [B][stride] for decode (`per_request`), the sequence's own entries for prefill.
   struct Table { const int32_t* p; int32_t n; };
@@ -373,6 +415,26 @@ NATIVE(prefill) {
   });
 }
 
+// ------------------------------------------------------------------------------------------------ around the attention
+// (ctx, x, gain, eps, out, residual, residual_out, out_e4m3, out_scale)
+NATIVE(rms_norm) {
+  Args a(args, nargs, 9);
+  if (!a.ok) return nullptr;
+  precc_ctx* ctx = a.ctx();
+  const Args::Matrix x = a.matrix("x", at::kBFloat16);
+  const int64_t n = x.rows * x.width;
+  void* gain = a.sized("gain", at::kBFloat16, x.width, true);
+  const float eps = a.f32();
+  void* out = a.sized("out", at::kBFloat16, n, false);
+  void* res = a.sized("residual", at::kBFloat16, n, false);
+  void* res_out = a.sized("residual_out", at::kBFloat16, n, false);
+  void* q = a.sized("out_e4m3", at::kFloat8_e4m3fn, n, false);
+  float* scale = static_cast<float*>(a.sized("out_scale", at::kFloat, x.rows, false));
+  if (!a.on_current_device()) return nullptr;
+  return finish(ctx, "precc_rms_norm", [&](void* st) {
+    return precc_rms_norm(ctx, x.p, res, gain, (int32_t)x.rows, (int32_t)x.width, eps, res_out, out, q, scale, st); });
+}
+
 // (error class, cache class) of binding.py
 PyObject* set_types(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 2) { PyErr_SetString(PyExc_TypeError, "set_types(error, cache)"); return nullptr; }
@@ -409,6 +471,7 @@ PyMethodDef methods[] = {
     FAST("lr_attend_decode_partial", decode_partial), FAST("combine_partials", combine_partials),
     FAST("lr_attend_prefill", prefill<PF_PLAIN>), FAST("lr_attend_prefill_ws", prefill<PF_WS>),
     FAST("lr_attend_prefill_rope", prefill<PF_ROPE>), FAST("lr_attend_prefill_rope_scratch", prefill<PF_SCRATCH>),
+    FAST("rms_norm", rms_norm),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of the precc calls.", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
