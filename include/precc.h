@@ -426,6 +426,47 @@ int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, cons
                        int32_t width, float eps, void* residual_out, void* out, void* out_e4m3,
                        float* out_scale, void* stream);
 
+/* The projection of a batch whose rows belong to different agents (query and output projections; Eq. 1 per row):
+ *   Y[m] = X[m] W + lora_scale * (X[m] A_a) B_a,   a = agent_id[m];   a = -1: X[m] W
+ *   X           [M][k_dim], Y [M][n_out]; rows of Y past M are not touched; Y must not overlap an input
+ *   W_packed    precc_pack_kmajor of W [k_dim][n_out] (dst_rows = n_out)
+ *   A_packed    precc_pack_kmajor of every A_a [k_dim][rank], a = 0, 1, ..: dst_rows = n_agents*rank, dst_row0 = a*rank
+ *   B           [n_agents][rank][n_out]
+ *   agent_id    [M] in [-1, n_agents); NULL: no row has an adapter (A_packed, B and ws may be NULL then, as with
+ *               rank 0).  A row with an id outside is computed without an adapter, and PRECC_STATUS_BAD_INDEX is recorded.
+ *   ws          device scratch of precc_adapted_ws_bytes(proj, M), 128-byte aligned, of any content; calls that may
+ *               run at the same time (also from two captured graphs) need separate ones
+ * X A is rounded to bf16 before it meets B; everything else is summed in fp32 and rounded once.  A row depends on its own row of
+ * X, W and its own agent's A and B alone, also where others hold infinities or NaN.  The order of the sums depends
+ * on M, the sizes and the device, not on the other rows' agents.
+ * 8 bits: X and W are e4m3, X[m] = x_scale[m] * X_e4m3[m] (as precc_rms_norm leaves it), W_packed and w_scale [n_out] from
+ * precc_pack_kmajor_e4m3; A stays bf16, B_packed comes from precc_pack_expand_e4m3.
+ * Supported: k_dim a multiple of 64 (8 bits: 128), n_out of 8, both up to 2^20; rank 0, 8, 16, 32 or 64; up to 64 agents;
+ * M up to 2^26.  M == 0 is a no-op. */
+typedef struct {
+  int32_t k_dim, n_out;
+  int32_t n_agents, rank;      /* rank 0: no adapters */
+  float lora_scale;
+} precc_projection;
+
+size_t precc_adapted_ws_bytes(const precc_projection* proj, int32_t M);
+int32_t precc_adapted_project(precc_ctx* ctx, const precc_projection* proj, const void* X, int32_t M,
+                              const void* W_packed, const void* A_packed, const void* B,
+                              const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream);
+int32_t precc_adapted_project_e4m3(precc_ctx* ctx, const precc_projection* proj, const void* X,
+                                   const float* x_scale, int32_t M, const void* W_packed,
+                                   const float* w_scale, const void* A_packed, const void* B_packed,
+                                   const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream);
+
+/* Weights in 8 bits.  src bf16 [k_dim][n_cols] -> dst e4m3 [k_dim/128][n_cols][128], scale [n_cols]: the least power of two
+ * (2^-100 at least) with which the largest magnitude of the column is at most 448; 1 for a column of zeros.
+ * Weights must be finite. */
+int32_t precc_pack_kmajor_e4m3(precc_ctx* ctx, const void* src, int32_t k_dim, int32_t n_cols, void* dst,
+                               float* scale, void* stream);
+/* B bf16 [rows][n_cols] -> dst = bf16(B / w_scale[column]) (exact for powers of two). */
+int32_t precc_pack_expand_e4m3(precc_ctx* ctx, const void* B, int32_t rows, int32_t n_cols, const float* w_scale,
+                               void* dst, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,8 @@ EXPORTS = [
     "precc_set_wait_limit", "precc_selftest_wait_timeout",
     "precc_prefill_rope_scratch_bytes", "precc_lr_attend_prefill_rope_scratch",
     "precc_prefill_ws_bytes", "precc_lr_attend_prefill_ws",
-    "precc_rms_norm",
+    "precc_rms_norm", "precc_adapted_ws_bytes", "precc_adapted_project", "precc_adapted_project_e4m3", "precc_pack_kmajor_e4m3",
+    "precc_pack_expand_e4m3",
 ]
 
 
@@ -54,6 +55,10 @@ _native = None
 
 class RopeDesc(C.Structure):
     _fields_ = [("table", C.c_void_p), ("max_pos", C.c_int32), ("positions", C.c_void_p), ("start_pos", C.c_int64)]
+
+
+class ProjectionDesc(C.Structure):
+    _fields_ = [("k_dim", C.c_int32), ("n_out", C.c_int32), ("n_agents", C.c_int32), ("rank", C.c_int32), ("lora_scale", C.c_float)]
 
 
 def load_library() -> C.CDLL:
@@ -119,6 +124,13 @@ def load_library() -> C.CDLL:
                                                    C.POINTER(CacheDesc), vp, vp, sz, vp]
     lib.precc_combine_partials.argtypes = [vp, C.POINTER(LayerDesc), vp, i32, i32, vp, vp, vp, vp]
     lib.precc_rms_norm.argtypes = [vp, vp, vp, vp, i32, i32, C.c_float, vp, vp, vp, vp, vp]
+    pd = C.POINTER(ProjectionDesc)
+    lib.precc_adapted_ws_bytes.argtypes = [pd, i32]
+    lib.precc_adapted_ws_bytes.restype = sz
+    lib.precc_adapted_project.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.precc_adapted_project_e4m3.argtypes = [vp, pd, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.precc_pack_kmajor_e4m3.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+    lib.precc_pack_expand_e4m3.argtypes = [vp, vp, i32, i32, vp, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int:  # default restype: the int32 status code
@@ -170,6 +182,14 @@ class Cache:
 
     def nbytes(self) -> int:
         return sum(t.numel() * 2 for t in (self.k_base, self.v_base, self.lr_k, self.lr_v) if t is not None)
+
+
+class AdaptedWeights:
+    """One projection with its agents' adapters as the kernels take it (see ``Precc.adapted_weights``)."""
+
+    def __init__(self, desc: ProjectionDesc, W: torch.Tensor, w_scale: Optional[torch.Tensor], A: Optional[torch.Tensor],
+                 B: Optional[torch.Tensor]):
+        self.desc, self.W, self.w_scale, self.A, self.B = desc, W, w_scale, A, B
 
 
 class Precc:
@@ -374,3 +394,49 @@ class Precc:
         """Norm of x (+ residual) over its last dimension: bf16 into ``out``, 8 bits with one fp32 scale per row into ``out_e4m3`` /
         ``out_scale``, the sum itself into ``residual_out`` (which may be ``residual``)."""
         _native.rms_norm(self._ctx, x, gain, eps, out, residual, residual_out, out_e4m3, out_scale)
+
+    def adapted_weights(self, W: torch.Tensor, A: Optional[torch.Tensor], B: Optional[torch.Tensor], scale: float,
+                        e4m3: bool = False) -> AdaptedWeights:
+        """W [k, n], A [agents, k, r], B [agents, r, n] (A and B None: no adapters), all bf16 -> laid out for ``adapted_project``, or with
+        ``e4m3`` quantised for ``adapted_project_e4m3``.  In bf16 B is used where it lies."""
+        if (A is None) != (B is None):
+            raise PreccError("A and B come together")
+        if W.dim() != 2 or W.dtype != torch.bfloat16:
+            raise PreccError("W must be bf16 [k, n]")
+        k, n = W.shape
+        agents, r = (A.shape[0], A.shape[2]) if A is not None and A.dim() == 3 else (0, 0)
+        if A is not None and (A.shape != (agents, k, r) or B.shape != (agents, r, n) or A.dtype != W.dtype or B.dtype != W.dtype):
+            raise PreccError("A must be bf16 [agents, k, r] and B bf16 [agents, r, n]")
+        w_scale = None
+        if e4m3:
+            packed = torch.empty((k // 128, n, 128), dtype=torch.float8_e4m3fn, device=W.device)
+            w_scale = torch.empty(n, dtype=torch.float32, device=W.device)
+            self._check(self.lib.precc_pack_kmajor_e4m3(self.h, _ptr(W), k, n, _ptr(packed), _ptr(w_scale), _stream()), "precc_pack_kmajor_e4m3")
+        else:
+            packed = torch.empty((n, k), dtype=torch.bfloat16, device=W.device)
+            self.pack_kmajor(W, packed, 0)
+        A_packed = None
+        if r:
+            A_packed = torch.empty((agents * r, k), dtype=torch.bfloat16, device=W.device)
+            for a in range(agents):
+                self.pack_kmajor(A[a], A_packed, a * r)
+            if e4m3:
+                B, src = torch.empty_like(B), B
+                self._check(self.lib.precc_pack_expand_e4m3(self.h, _ptr(src), agents * r, n, _ptr(w_scale), _ptr(B), _stream()),
+                            "precc_pack_expand_e4m3")
+        return AdaptedWeights(ProjectionDesc(k, n, agents, r, scale), packed, w_scale, A_packed, B if r else None)
+
+    def adapted_workspace(self, weights: AdaptedWeights, max_rows: int) -> Optional[torch.Tensor]:
+        """Scratch for calls of up to max_rows rows (None where the projection has no adapters)."""
+        n = self.lib.precc_adapted_ws_bytes(C.byref(weights.desc), max_rows)
+        return torch.empty(n, dtype=torch.uint8, device=f"cuda:{self.device}") if n else None
+
+    def adapted_project(self, weights: AdaptedWeights, x: torch.Tensor, out: torch.Tensor, agent_id: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None):
+        """out[m] = x[m] W + scale (x[m] A_a) B_a with a = agent_id[m] (int32; -1 or no ``agent_id``: the shared weights alone)."""
+        _native.adapted_project(self._ctx, weights, x, out, agent_id, workspace)
+
+    def adapted_project_e4m3(self, weights: AdaptedWeights, x: torch.Tensor, x_scale: torch.Tensor, out: torch.Tensor,
+                             agent_id: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+        """The same from 8-bit rows x with one fp32 scale each (what ``rms_norm`` writes) and 8-bit weights."""
+        _native.adapted_project_e4m3(self._ctx, weights, x, x_scale, out, agent_id, workspace)

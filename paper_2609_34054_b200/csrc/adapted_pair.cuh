@@ -1,0 +1,228 @@
+// The main kernel of the adapted projection for many rows: persistent pairs of SMs, 256 rows x BN columns a tile (tcgen05 cta_group::2,
+// two accumulators in tensor memory).  The ring, its hand-offs and the tile walk are those of the pair form of the plain projection GEMM.
+//
+// The adapters are more K: behind the last step of W a tile takes one step of depth rank_pad for every agent among its rows, with
+// T rows as the A operand and that agent's B (columns contiguous in memory, so an MN-major operand) as the other.  The rows of a tile
+// are the lanes of the accumulator, and the MMA leaves the lanes of other agents' rows alone (its lane mask): no other adapter, were it
+// infinite or NaN, touches a row, and T needs no zeros for the rows of others.
+#pragma once
+#include "adapted.cuh"
+
+namespace precc {
+
+constexpr int AP_THREADS = 192;                       // producer, MMA issuer, four epilogue warps
+constexpr int AP_BM = 2 * GEMM_BM;
+constexpr int AP_A_BYTES = GEMM_BM * AP_ROW_BYTES;
+
+__host__ __device__ constexpr int ap_w_bytes(int bn) { return (bn / 2 + 63) / 64 * 64 * AP_ROW_BYTES; }   // (a step of B takes whole boxes of 64 columns)
+__host__ __device__ constexpr int ap_stage_bytes(int bn) { return AP_A_BYTES + ap_w_bytes(bn); }
+
+__device__ __forceinline__ void umma_pair_e4m3(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n"
+      ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+// D += A B on the lanes whose bit in `off` is clear.
+__device__ __forceinline__ void umma_pair_bf16_lanes(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, const uint32_t (&off)[8]) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, 1, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%4, %5, %6, %7, %8, %9, %10, %11}, p;\n\t}\n"
+      ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3]), "r"(off[4]), "r"(off[5]),
+        "r"(off[6]), "r"(off[7]) : "memory");
+}
+
+template <bool Q8>
+__global__ void __launch_bounds__(AP_THREADS, 1)
+adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                    const __grid_constant__ CUtensorMap map_t, const __grid_constant__ CUtensorMap map_b, const AdaptedParams p) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const int half_n = p.BN / 2;
+  const int stage_bytes = ap_stage_bytes(p.BN);
+  const uint32_t step_tx = 2u * (AP_A_BYTES + half_n * AP_ROW_BYTES);
+  const int b_boxes = (half_n + 63) / 64;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)p.stages * stage_bytes);
+  const uint32_t full0 = smem_u32(bars);
+  const uint32_t empty0 = full0 + 8 * p.stages;
+  const uint32_t acc_full = empty0 + 8 * p.stages;
+  const uint32_t acc_empty = acc_full + 16;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bars + 2 * p.stages + 4);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int nkb = p.K / (Q8 ? 128 : 64);
+  const int n_tiles_n = (p.N + p.BN - 1) / p.BN;
+  const long long n_tiles = (long long)((p.M + AP_BM - 1) / AP_BM) * n_tiles_n;
+  const bool adapters = p.agent_id != nullptr;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+    mbar_init(acc_full, 1); mbar_init(acc_full + 8, 1);
+    mbar_init(acc_empty, 8); mbar_init(acc_empty + 8, 8);
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tmem_holder)), "r"(p.tmem_cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+  }
+  if (!adapters) pdl_wait();       // with adapters the kernel ahead is the shrink kernel, which starts this one behind its own wait
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  pair_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+  const uint32_t tmem_base = *tmem_holder;
+  if (!adapters) pdl_launch_dependents();
+
+  // the agents among the 256 rows of a tile, one bit each; `id[i]` is the agent of row 32 i + lane
+  auto agents_of = [&](long long m0, int (&id)[8]) -> unsigned long long {
+    unsigned lo = 0, hi = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      id[i] = agent_of(p, m0 + 32 * i + lane);
+      if (id[i] >= 0) { if (id[i] < 32) lo |= 1u << id[i]; else hi |= 1u << (id[i] - 32); }
+    }
+    return (static_cast<unsigned long long>(__reduce_or_sync(0xffffffffu, hi)) << 32) | __reduce_or_sync(0xffffffffu, lo);
+  };
+
+  if (warp == 0) {
+    const uint32_t full0_lead = map_to_rank(full0, 0);
+    int it = 0;
+    bool waited = false;
+    for (long long t = pair; t < n_tiles; t += n_pairs) {
+      const int mt = (int)(t / n_tiles_n) * AP_BM;
+      const int m0 = mt + (int)rank * GEMM_BM, n0 = (int)(t % n_tiles_n) * p.BN + (int)rank * half_n;
+      int id[8];
+      unsigned long long present = adapters ? agents_of(mt, id) : 0ull;
+      if (lane == 0) {
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const int s = it % p.stages;
+          if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
+          const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes);
+          if (rank == 0) mbar_expect_tx(full0 + 8 * s, step_tx);
+          tma_pair_load_2d(sa, &map_x, kb * (Q8 ? 128 : 64), m0, full0_lead + 8 * s);
+          tma_pair_load_3d(sa + AP_A_BYTES, &map_w, 0, n0, kb, full0_lead + 8 * s);
+        }
+        if (adapters && !waited) {       // T is complete; also with no adapter in this tile, so that this grid ends after the shrink kernel
+          pdl_wait();
+          pdl_launch_dependents();
+          waited = true;
+        }
+        for (; present; present &= present - 1, ++it) {
+          const int a = __ffsll(present) - 1;
+          const int s = it % p.stages;
+          if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
+          const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes);
+          if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2u * (GEMM_BM + b_boxes * 64) * p.rank_pad * 2);
+          tma_pair_load_2d(sa, &map_t, 0, m0, full0_lead + 8 * s);
+          for (int j = 0; j < b_boxes; ++j)
+            tma_pair_load_3d(sa + AP_A_BYTES + j * p.rank_pad * 128, &map_b, n0 + 64 * j, 0, a, full0_lead + 8 * s);
+        }
+      }
+      __syncwarp();
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const uint32_t idesc = Q8 ? umma_pair_idesc_bf16(p.BN) & ~((1u << 7) | (1u << 10)) : umma_pair_idesc_bf16(p.BN);   // (e4m3 is format 0)
+      const uint32_t idesc_b = umma_pair_idesc_bf16(p.BN) | (1u << 16);                                                 // B operand MN-major
+      const uint64_t da0 = umma_desc_sw128(smem_u32(smem));
+      const uint64_t db0 = umma_desc_sw128(smem_u32(smem) + AP_A_BYTES);
+      const uint64_t dt0 = umma_desc_kmajor(smem_u32(smem), p.rank_pad * 2);
+      const uint64_t de0 = umma_desc_mnmajor(smem_u32(smem) + AP_A_BYTES, 128, p.rank_pad * 128);
+      int it = 0, i = 0;
+      for (long long t = pair; t < n_tiles; t += n_pairs, ++i) {
+        const int buf = i & 1;
+        const int mt = (int)(t / n_tiles_n) * AP_BM;
+        int id[8];
+        unsigned long long present = adapters ? agents_of(mt, id) : 0ull;
+        const uint32_t d = tmem_base + buf * p.BN;
+        if (lane == 0) {
+          if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          for (int kb = 0; kb < nkb; ++kb) {
+            const int s = (it + kb) % p.stages;
+            mbar_wait(full0 + 8 * s, ((it + kb) / p.stages) & 1, p.status);
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+            const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {             // 32 bytes of K a step: 16 bf16 or 32 e4m3
+              if constexpr (Q8) umma_pair_e4m3(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
+              else umma_pair_bf16(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
+            }
+            umma_pair_commit_both(empty0 + 8 * s);
+          }
+        }
+        it += nkb;
+        __syncwarp();
+        for (; present; present &= present - 1, ++it) {
+          const int a = __ffsll(present) - 1;
+          uint32_t off[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) off[j] = ~__ballot_sync(0xffffffffu, id[j] == a);
+          if (lane == 0) {
+            const int s = it % p.stages;
+            mbar_wait(full0 + 8 * s, (it / p.stages) & 1, p.status);
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+            const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
+            for (int k = 0; k < p.rank_pad / 16; ++k)
+              umma_pair_bf16_lanes(d, dt0 + so + 2 * k, de0 + so + 128 * k, idesc_b, off);
+            umma_pair_commit_both(empty0 + 8 * s);
+          }
+          __syncwarp();
+        }
+        if (lane == 0) umma_pair_commit_both(acc_full + 8 * buf);
+        __syncwarp();
+      }
+    }
+  } else {
+    const int lane_base = (warp & 3) * 32;
+    const uint32_t acc_empty_lead = map_to_rank(acc_empty, 0);
+    int i = 0;
+    for (long long t = pair; t < n_tiles; t += n_pairs, ++i) {
+      const int buf = i & 1;
+      const int m = (int)(t / n_tiles_n) * AP_BM + (int)rank * GEMM_BM + lane_base + lane, n0 = (int)(t % n_tiles_n) * p.BN;
+      const bool row_ok = m < p.M;
+      float xs = 1.f;
+      if constexpr (Q8) xs = row_ok ? p.x_scale[m] : 0.f;
+      __nv_bfloat16* yr = p.y + (long long)m * p.N + n0;
+      mbar_wait_relaxed(acc_full + 8 * buf, (i >> 1) & 1, p.status);
+      asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+      const uint32_t acc = tmem_base + buf * p.BN + (static_cast<uint32_t>(lane_base) << 16);
+      for (int c0 = 0; c0 < p.BN && n0 + c0 < p.N; c0 += 16) {
+        uint32_t r[16];
+        tmem_ld16(acc + c0, r);
+        asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (!row_ok || n0 + c0 + 8 * h >= p.N) continue;       // (N is a multiple of 8)
+          float v[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[8 * h + k]);
+          if constexpr (Q8) {
+            const float4* ws = reinterpret_cast<const float4*>(p.w_scale + n0 + c0 + 8 * h);
+            const float4 u = __ldg(ws), w = __ldg(ws + 1);
+            v[0] *= xs * u.x; v[1] *= xs * u.y; v[2] *= xs * u.z; v[3] *= xs * u.w;
+            v[4] *= xs * w.x; v[5] *= xs * w.y; v[6] *= xs * w.z; v[7] *= xs * w.w;
+          }
+          *reinterpret_cast<uint4*>(yr + c0 + 8 * h) = pack_bf16x8(v);
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+      __syncwarp();
+      if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(acc_empty_lead + 8 * buf) : "memory");
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  pair_sync();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base), "r"(p.tmem_cols) : "memory");
+  }
+}
+
+}  // namespace precc

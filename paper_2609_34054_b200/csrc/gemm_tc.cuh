@@ -284,11 +284,6 @@ proj_gemm_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
   }
 }
 
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr));
-}
 // position of a row in the rotary table, or -1 (reported) when it is outside
 __device__ __forceinline__ long long rope_pos(const GemmParams& p, int gm) {
   const long long pos = p.positions ? (long long)p.positions[gm] : p.start_pos + gm;

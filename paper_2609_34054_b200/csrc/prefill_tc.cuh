@@ -168,31 +168,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
 
-// layout_type field of a shared-memory matrix descriptor for rows of `row_bytes`
-__device__ __forceinline__ constexpr uint64_t umma_layout_for(int row_bytes) {
-  return row_bytes >= 128 ? 2ull : (row_bytes == 64 ? 4ull : 6ull);
-}
-// K-major operand: rows of `row_bytes` (one swizzle span), 8-row groups `8*row_bytes` apart.
-__device__ __forceinline__ uint64_t umma_desc_kmajor(uint32_t saddr, int row_bytes) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFF) >> 4);
-  d |= static_cast<uint64_t>(1) << 16;
-  d |= static_cast<uint64_t>((8 * row_bytes) >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= umma_layout_for(row_bytes) << 61;
-  return d;
-}
-// MN-major operand (rows = k index, `row_bytes` of contiguous MN elements per row): 8-row groups
-// `8*row_bytes` apart (stride offset), successive MN blocks `mn_block_stride` bytes apart (leading offset).
-__device__ __forceinline__ uint64_t umma_desc_mnmajor(uint32_t saddr, int row_bytes, int mn_block_stride) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFF) >> 4);
-  d |= static_cast<uint64_t>((mn_block_stride >> 4) & 0x3FFF) << 16;
-  d |= static_cast<uint64_t>((8 * row_bytes) >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= umma_layout_for(row_bytes) << 61;
-  return d;
-}
 // D fp32, A/B bf16, M = 128, N = n; b_mn = 1 when B is MN-major.
 __device__ __forceinline__ uint32_t umma_idesc(int n, int b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(b_mn) << 16) | (static_cast<uint32_t>(n >> 3) << 17) |

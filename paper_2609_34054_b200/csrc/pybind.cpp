@@ -22,7 +22,7 @@ namespace {
 
 PyObject* g_error = nullptr;   // binding.PreccError
 PyObject* g_cache = nullptr;   // binding.Cache
-PyObject *s_desc, *s_k_base, *s_v_base, *s_lr_k, *s_lr_v, *s_n_blocks;
+PyObject *s_desc, *s_k_base, *s_v_base, *s_lr_k, *s_lr_v, *s_n_blocks, *s_W, *s_A, *s_B, *s_w_scale;
 
 // One call's arguments, taken in order; the first problem sets the Python error and makes the rest no-ops.
 struct Args {
@@ -79,8 +79,13 @@ struct Args {
   }
   // A tensor of a given type and number of elements (None where `required` is false).  The calls around the attention take their
   // sizes from the tensors, so that no size can disagree with a buffer, and want them all on one device, the current one.
-  void* sized(const char* name, c10::ScalarType type, int64_t n, bool required) {
-    const at::Tensor* t = tensor();
+  void* sized(const char* name, c10::ScalarType type, int64_t n, bool required) { return sized(tensor(), name, type, n, required); }
+  void* member_sized(PyObject* o, PyObject* attr, const char* name, c10::ScalarType type, int64_t n, bool required) {
+    THPObjectPtr m(ok ? PyObject_GetAttr(o, attr) : nullptr);   // (the object still holds it afterwards)
+    if (!m) { ok = false; return nullptr; }
+    return sized(tensor(m), name, type, n, required);
+  }
+  void* sized(const at::Tensor* t, const char* name, c10::ScalarType type, int64_t n, bool required) {
     if (!ok) return nullptr;
     if (!t) {
       if (required) { PyErr_Format(g_error, "%s is None", name); ok = false; }
@@ -435,6 +440,37 @@ NATIVE(rms_norm) {
     return precc_rms_norm(ctx, x.p, res, gain, (int32_t)x.rows, (int32_t)x.width, eps, res_out, out, q, scale, st); });
 }
 
+// (ctx, weights, x, [x_scale,] out, agent_id, workspace); weights: binding.AdaptedWeights, read member by member
+template <bool Q8>
+NATIVE(adapted_project) {
+  Args a(args, nargs, Q8 ? 7 : 6);
+  if (!a.ok) return nullptr;
+  precc_ctx* ctx = a.ctx();
+  PyObject* w = a.next();
+  precc_projection d = {};
+  THPObjectPtr dp(PyObject_GetAttr(w, s_desc));
+  if (!dp) return nullptr;
+  a.copy(dp, &d, sizeof(d), "weights.desc is not a ProjectionDesc");
+  if (!a.ok) return nullptr;
+  const int64_t n_agents = d.n_agents, low = n_agents * d.rank;
+  const Args::Matrix x = a.matrix("x", Q8 ? at::kFloat8_e4m3fn : at::kBFloat16);
+  if (a.ok && x.width != d.k_dim) { PyErr_Format(g_error, "x has %lld columns, the projection takes %d", (long long)x.width, (int)d.k_dim); return nullptr; }
+  float* xs = Q8 ? static_cast<float*>(a.sized("x_scale", at::kFloat, x.rows, true)) : nullptr;
+  void* out = a.sized("out", at::kBFloat16, x.rows * d.n_out, true);
+  const int32_t* agent = static_cast<const int32_t*>(a.sized("agent_id", at::kInt, x.rows, false));
+  const at::Tensor* wst = a.tensor();
+  const Args::Buffer ws = a.buffer(wst);
+  void* W = a.member_sized(w, s_W, "weights.W", Q8 ? at::kFloat8_e4m3fn : at::kBFloat16, (int64_t)d.k_dim * d.n_out, true);
+  void* A = a.member_sized(w, s_A, "weights.A", at::kBFloat16, low * d.k_dim, low > 0);
+  void* B = a.member_sized(w, s_B, "weights.B", at::kBFloat16, low * d.n_out, low > 0);
+  float* wsc = Q8 ? static_cast<float*>(a.member_sized(w, s_w_scale, "weights.w_scale", at::kFloat, d.n_out, true)) : nullptr;
+  if (wst && a.ok && wst->get_device() != a.device) a.bad("workspace is on another device than the tensors before it");
+  if (!a.on_current_device()) return nullptr;
+  return finish(ctx, Q8 ? "precc_adapted_project_e4m3" : "precc_adapted_project", [&](void* st) {
+    if (Q8) return precc_adapted_project_e4m3(ctx, &d, x.p, xs, (int32_t)x.rows, W, wsc, A, B, agent, out, ws.p, ws.bytes, st);
+    return precc_adapted_project(ctx, &d, x.p, (int32_t)x.rows, W, A, B, agent, out, ws.p, ws.bytes, st); });
+}
+
 // (error class, cache class) of binding.py
 PyObject* set_types(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 2) { PyErr_SetString(PyExc_TypeError, "set_types(error, cache)"); return nullptr; }
@@ -471,7 +507,7 @@ PyMethodDef methods[] = {
     FAST("lr_attend_decode_partial", decode_partial), FAST("combine_partials", combine_partials),
     FAST("lr_attend_prefill", prefill<PF_PLAIN>), FAST("lr_attend_prefill_ws", prefill<PF_WS>),
     FAST("lr_attend_prefill_rope", prefill<PF_ROPE>), FAST("lr_attend_prefill_rope_scratch", prefill<PF_SCRATCH>),
-    FAST("rms_norm", rms_norm),
+    FAST("rms_norm", rms_norm), FAST("adapted_project", adapted_project<false>), FAST("adapted_project_e4m3", adapted_project<true>),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of the precc calls.", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
@@ -485,6 +521,10 @@ PyMODINIT_FUNC PyInit__native() {
   s_lr_k = PyUnicode_InternFromString("lr_k");
   s_lr_v = PyUnicode_InternFromString("lr_v");
   s_n_blocks = PyUnicode_InternFromString("n_blocks");
+  s_W = PyUnicode_InternFromString("W");
+  s_A = PyUnicode_InternFromString("A");
+  s_B = PyUnicode_InternFromString("B");
+  s_w_scale = PyUnicode_InternFromString("w_scale");
   Py_INCREF(PyExc_RuntimeError);
   g_error = PyExc_RuntimeError;
   return PyModule_Create(&module_def);
