@@ -30,6 +30,7 @@ struct AdaptedParams {
   __nv_bfloat16* T;                           // [M][rank_pad]
   __nv_bfloat16* y;                           // [M][N]
   float s;
+  int tile_rows;                              // shrink kernel: rows of a block
   int BN, stages, tmem_cols;
   uint32_t* status;
 };
@@ -57,7 +58,7 @@ __device__ __forceinline__ void e4m3x8_to_bf16(uint32_t lo, uint32_t hi, uint32_
 constexpr int SHRINK_WARPS = 8;
 constexpr int SHRINK_THREADS = SHRINK_WARPS * 32;
 
-// T of 8 NT rows.  MT: 16-wide pieces of the rank.  The K extent is split over the warps of a block and the blocks of a cluster;
+// T of up to 8 NT rows (fewer where that fills more SMs: a block takes the agents among its rows one after the other).  MT: 16-wide pieces of the rank.  The K extent is split over the warps of a block and the blocks of a cluster;
 // partial sums meet in shared memory in a fixed order.  The rows are the N axis of mma.sync and the coordinates of the rank its M axis, so a row
 // is computed in its own column of the product and nothing of another agent's adapter reaches it: for every agent among the rows
 // the product is taken with the rows of that agent (the others' columns are zero and dropped).
@@ -73,12 +74,12 @@ adapted_shrink_kernel(const AdaptedParams p) {
   asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank_c));
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;\n" : "=r"(KS));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const long long row0 = (long long)(blockIdx.x / KS) * RT;
+  const long long row0 = (long long)(blockIdx.x / KS) * p.tile_rows;
   pdl_wait();
   pdl_launch_dependents();
 
   int id = -1;
-  if (lane < RT && row0 + lane < p.M) {
+  if (lane < p.tile_rows && row0 + lane < p.M) {
     const int raw = p.agent_id[row0 + lane];
     if (raw < -1 || raw >= p.n_agents) { if (warp == 0 && rank_c == 0) atomicOr(p.status, StatusBits::BAD_INDEX); }
     else id = raw;

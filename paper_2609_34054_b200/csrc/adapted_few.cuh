@@ -1,0 +1,188 @@
+// The main kernel of the adapted projection for a handful of rows (decode steps, up to 16): one pass over the weights.
+//
+// HBM-bound at K x N weights.  A block takes 16 MT output columns over the whole K extent, its eight warps every eighth k-block
+// (so nothing is merged between blocks), and each warp asks for several k-blocks of weights before it uses the first: the
+// fragments of mma.sync come straight from the packed weights into registers, 16 bytes a lane, which keeps more of the matrix in
+// flight than a ring in shared memory would.  Output columns are the M axis of the MMA and the rows of X its N axis, so
+// eight rows cost nothing over one.
+// The adapters: warp u takes the u-th agent among the rows.  Its B slice (r x 16 MT) is asked for with the first weights and meets that agent's rows
+// of T once the shrink kernel is done; the rows of others are zero in the product and dropped from it.
+#pragma once
+#include "adapted.cuh"
+
+namespace precc {
+
+constexpr int AF_WARPS = 8;
+constexpr int AF_THREADS = AF_WARPS * 32;
+constexpr int AF_MAX_ROWS = 16;
+
+// D(16x8, fp32) += A(16x32, e4m3, row) * B(32x8, e4m3, col)
+__device__ __forceinline__ void mma_e4m3_16832(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Weights are read once: past L1.
+__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+__host__ __device__ constexpr int af_smem_bytes(int nt, int mt, int rank_pad) {
+  return (AF_WARPS + 1) * 8 * nt * (16 * mt + 4) * 4 + AF_WARPS * rank_pad * (32 * mt + 16);
+}
+
+// NT: eight-row pieces of X.  MT: sixteen-column pieces of a block.  Steps of 128 bytes of K (64 bf16, 128 e4m3).
+template <int NT, int MT, bool Q8>
+__global__ void __launch_bounds__(AF_THREADS, MT == 1 ? 2 : 1)
+adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
+  constexpr int C = 16 * MT, S = C + 4;           // row of the partial sums, padded: the lanes of a store hit 32 banks
+  constexpr int BP = C * 2 + 16;                  // bytes of a row of a B slice, padded for ldmatrix
+  constexpr int U = MT == 1 && NT == 2 ? 2 : 3;   // k-blocks of a warp in flight
+  extern __shared__ __align__(16) uint8_t smem[];
+  float (*red)[8 * NT][S] = reinterpret_cast<float (*)[8 * NT][S]>(smem);                    // [warp]
+  float (*low)[S] = red[AF_WARPS];                                                           // s (x A) B of every row
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t b_s = smem_u32(smem) + (AF_WARPS + 1) * 8 * NT * S * 4 + warp * p.rank_pad * BP;      // this warp's slice of B
+  const int n0 = blockIdx.x * C;
+  const bool adapters = p.agent_id != nullptr;
+  if (!adapters) { pdl_wait(); pdl_launch_dependents(); }      // with adapters the shrink kernel is ahead and has waited
+
+  const int nkb = p.K / (Q8 ? 128 : 64);
+  const long long row_bytes = (long long)p.K * (Q8 ? 1 : 2);
+  const uint8_t* x = static_cast<const uint8_t*>(p.x);
+  float acc[MT][NT][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) { acc[m][n][0] = acc[m][n][1] = acc[m][n][2] = acc[m][n][3] = 0.f; }
+  uint4 wv[U][MT][2][2], xv[U][NT][2];            // [..][row g, row g + 8][piece t, piece t + 4]
+  auto fetch = [&](int u, int kb) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int n = n0 + m * 16 + h * 8 + g;
+        const uint4* src = reinterpret_cast<const uint4*>(W + ((long long)kb * p.N + n) * AP_ROW_BYTES);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) wv[u][m][h][c] = kb < nkb && n < p.N ? ld_stream(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint4* src = reinterpret_cast<const uint4*>(x + (n * 8 + g) * row_bytes + (long long)kb * AP_ROW_BYTES);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) xv[u][n][c] = kb < nkb && n * 8 + g < p.M ? __ldg(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) fetch(u, warp + u * AF_WARPS);
+
+  // this warp's agents (the w-th and the w + 8-th among the rows), and their slices of B
+  int id = -1;
+  if (adapters && lane < p.M) id = agent_of(p, lane);
+  unsigned todo = __ballot_sync(0xffffffffu, id >= 0);
+  const unsigned with_adapter = todo;
+  unsigned mine[NT];
+  int agent[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) { mine[i] = 0; agent[i] = -1; }
+  for (int u = 0; todo; ++u) {
+    const int a = __shfl_sync(0xffffffffu, id, __ffs(todo) - 1);
+    const unsigned same = __ballot_sync(0xffffffffu, id == a);
+    todo &= ~same;
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+      if (u == warp + i * AF_WARPS) { mine[i] = same; agent[i] = a; }
+  }
+  auto fetch_b = [&](int a) {                     // (coordinates past the rank, columns past N: zeros)
+    for (int i = lane; i < p.rank_pad * (C / 8); i += 32) {
+      const int r = i / (C / 8), c = i % (C / 8) * 8;
+      const bool on = r < p.rank && n0 + c < p.N;
+      cp_async16(b_s + r * BP + c * 2, on ? p.B + ((long long)a * p.rank + r) * p.N + n0 + c : p.B, on ? 16 : 0);
+    }
+    cp_async_commit();
+  };
+  if (agent[0] >= 0) fetch_b(agent[0]);
+
+  for (int kb = warp; kb < nkb; kb += U * AF_WARPS) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const uint32_t a0[4] = {wv[u][m][0][c].x, wv[u][m][1][c].x, wv[u][m][0][c].y, wv[u][m][1][c].y};
+          const uint32_t a1[4] = {wv[u][m][0][c].z, wv[u][m][1][c].z, wv[u][m][0][c].w, wv[u][m][1][c].w};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (Q8) {
+              mma_e4m3_16832(acc[m][n], a0, xv[u][n][c].x, xv[u][n][c].y);
+              mma_e4m3_16832(acc[m][n], a1, xv[u][n][c].z, xv[u][n][c].w);
+            } else {
+              mma_bf16_16816(acc[m][n], a0, xv[u][n][c].x, xv[u][n][c].y);
+              mma_bf16_16816(acc[m][n], a1, xv[u][n][c].z, xv[u][n][c].w);
+            }
+          }
+        }
+      fetch(u, kb + (u + U) * AF_WARPS);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) red[warp][n * 8 + 2 * t + (e & 1)][m * 16 + g + 8 * (e >> 1)] = acc[m][n][e];
+
+  if (adapters) {
+    pdl_wait();                                   // T is complete
+    if (threadIdx.x == 0) pdl_launch_dependents();
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      if (agent[i] < 0) continue;                 // (the same in every lane)
+      if (i > 0) { __syncwarp(); fetch_b(agent[i]); }
+      cp_async_wait<0>();
+      __syncwarp();
+      float d[C / 8][4];
+#pragma unroll
+      for (int j = 0; j < C / 8; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
+      for (int k0 = 0; k0 < p.rank_pad; k0 += 16) {
+        uint32_t a[4];                            // rows g and g + 8 of T, coordinates 2t.. and 2t + 8..
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r = g + 8 * (q & 1);
+          const __nv_bfloat16* src = p.T + (long long)r * p.rank_pad + k0 + 2 * t + 8 * (q >> 1);
+          a[q] = (mine[i] >> r) & 1u ? *reinterpret_cast<const uint32_t*>(src) : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < C / 16; ++j) {
+          uint32_t b[4];                          // 16 coordinates x 16 columns
+          ldsm_x4_t(b, b_s + (k0 + (lane & 15)) * BP + j * 32 + (lane >> 4) * 16);
+          mma_bf16_16816(d[2 * j], a, b[0], b[1]);
+          mma_bf16_16816(d[2 * j + 1], a, b[2], b[3]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < C / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = g + 8 * (e >> 1);
+          if ((mine[i] >> r) & 1u) low[r][8 * j + 2 * t + (e & 1)] = d[j][e];
+        }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.M * C; i += AF_THREADS) {
+    const int r = i / C, c = i % C;
+    if (n0 + c >= p.N) continue;
+    float v = (with_adapter >> r) & 1u ? low[r][c] : 0.f;
+#pragma unroll
+    for (int w = 0; w < AF_WARPS; ++w) v += red[w][r][c];
+    if constexpr (Q8) v *= __ldg(p.x_scale + r) * __ldg(p.w_scale + n0 + c);
+    p.y[(long long)r * p.N + n0 + c] = __float2bfloat16(v);
+  }
+}
+
+}  // namespace precc

@@ -40,6 +40,7 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     const __grid_constant__ CUtensorMap map_t, const __grid_constant__ CUtensorMap map_b, const AdaptedParams p) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const uint32_t smem0 = smem_u32(smem);
   const int half_n = p.BN / 2;
   const int stage_bytes = ap_stage_bytes(p.BN);
   const uint32_t step_tx = 2u * (AP_A_BYTES + half_n * AP_ROW_BYTES);
@@ -98,41 +99,44 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       const int m0 = mt + (int)rank * GEMM_BM, n0 = (int)(t % n_tiles_n) * p.BN + (int)rank * half_n;
       int id[8];
       unsigned long long present = adapters ? agents_of(mt, id) : 0ull;
-      if (lane == 0) {
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
-          const int s = it % p.stages;
-          if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
-          const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes);
+      for (int kb = 0; kb < nkb; ++kb, ++it) {
+        const int s = it % p.stages;
+        if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
+        const uint32_t sa = smem0 + s * stage_bytes;
+        if (elect_one()) {
           if (rank == 0) mbar_expect_tx(full0 + 8 * s, step_tx);
           tma_pair_load_2d(sa, &map_x, kb * (Q8 ? 128 : 64), m0, full0_lead + 8 * s);
           tma_pair_load_3d(sa + AP_A_BYTES, &map_w, 0, n0, kb, full0_lead + 8 * s);
         }
-        if (adapters && !waited) {       // T is complete; also with no adapter in this tile, so that this grid ends after the shrink kernel
-          pdl_wait();
-          pdl_launch_dependents();
-          waited = true;
-        }
-        for (; present; present &= present - 1, ++it) {
-          const int a = __ffsll(present) - 1;
-          const int s = it % p.stages;
-          if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
-          const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes);
+        __syncwarp();
+      }
+      if (adapters && !waited) {       // T is complete; also with no adapter in this tile, so that this grid ends after the shrink kernel
+        pdl_wait();
+        pdl_launch_dependents();
+        waited = true;
+      }
+      for (; present; present &= present - 1, ++it) {
+        const int a = __ffsll(present) - 1;
+        const int s = it % p.stages;
+        if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
+        const uint32_t sa = smem0 + s * stage_bytes;
+        if (elect_one()) {
           if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2u * (GEMM_BM + b_boxes * 64) * p.rank_pad * 2);
           tma_pair_load_2d(sa, &map_t, 0, m0, full0_lead + 8 * s);
           for (int j = 0; j < b_boxes; ++j)
             tma_pair_load_3d(sa + AP_A_BYTES + j * p.rank_pad * 128, &map_b, n0 + 64 * j, 0, a, full0_lead + 8 * s);
         }
+        __syncwarp();
       }
-      __syncwarp();
     }
   } else if (warp == 1) {
     if (rank == 0) {
       const uint32_t idesc = Q8 ? umma_pair_idesc_bf16(p.BN) & ~((1u << 7) | (1u << 10)) : umma_pair_idesc_bf16(p.BN);   // (e4m3 is format 0)
       const uint32_t idesc_b = umma_pair_idesc_bf16(p.BN) | (1u << 16);                                                 // B operand MN-major
-      const uint64_t da0 = umma_desc_sw128(smem_u32(smem));
-      const uint64_t db0 = umma_desc_sw128(smem_u32(smem) + AP_A_BYTES);
-      const uint64_t dt0 = umma_desc_kmajor(smem_u32(smem), p.rank_pad * 2);
-      const uint64_t de0 = umma_desc_mnmajor(smem_u32(smem) + AP_A_BYTES, 128, p.rank_pad * 128);
+      const uint64_t da0 = umma_desc_sw128(smem0);
+      const uint64_t db0 = umma_desc_sw128(smem0 + AP_A_BYTES);
+      const uint64_t dt0 = umma_desc_kmajor(smem0, p.rank_pad * 2);
+      const uint64_t de0 = umma_desc_mnmajor(smem0 + AP_A_BYTES, 128, p.rank_pad * 128);
       int it = 0, i = 0;
       for (long long t = pair; t < n_tiles; t += n_pairs, ++i) {
         const int buf = i & 1;
@@ -140,13 +144,13 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         int id[8];
         unsigned long long present = adapters ? agents_of(mt, id) : 0ull;
         const uint32_t d = tmem_base + buf * p.BN;
-        if (lane == 0) {
-          if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
+        if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
+        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const int s = it % p.stages;
+          mbar_wait(full0 + 8 * s, (it / p.stages) & 1, p.status);
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-          for (int kb = 0; kb < nkb; ++kb) {
-            const int s = (it + kb) % p.stages;
-            mbar_wait(full0 + 8 * s, ((it + kb) / p.stages) & 1, p.status);
-            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          if (elect_one()) {
             const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {             // 32 bytes of K a step: 16 bf16 or 32 e4m3
@@ -155,18 +159,17 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             }
             umma_pair_commit_both(empty0 + 8 * s);
           }
+          __syncwarp();
         }
-        it += nkb;
-        __syncwarp();
         for (; present; present &= present - 1, ++it) {
           const int a = __ffsll(present) - 1;
           uint32_t off[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) off[j] = ~__ballot_sync(0xffffffffu, id[j] == a);
-          if (lane == 0) {
-            const int s = it % p.stages;
-            mbar_wait(full0 + 8 * s, (it / p.stages) & 1, p.status);
-            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          const int s = it % p.stages;
+          mbar_wait(full0 + 8 * s, (it / p.stages) & 1, p.status);
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          if (elect_one()) {
             const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
             for (int k = 0; k < p.rank_pad / 16; ++k)
               umma_pair_bf16_lanes(d, dt0 + so + 2 * k, de0 + so + 128 * k, idesc_b, off);
@@ -174,7 +177,7 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
           }
           __syncwarp();
         }
-        if (lane == 0) umma_pair_commit_both(acc_full + 8 * buf);
+        if (elect_one()) umma_pair_commit_both(acc_full + 8 * buf);
         __syncwarp();
       }
     }

@@ -1,7 +1,9 @@
 // libprecc: the projection of a batch whose rows carry adapters of their own, in bf16 and in 8 bits, and the packing of 8-bit weights.
 #include <algorithm>
 
+#include "adapted_few.cuh"
 #include "adapted_pair.cuh"
+#include "adapted_turn.cuh"
 #include "api_internal.h"
 
 using namespace precc;
@@ -97,10 +99,12 @@ struct Launch {
 };
 
 template <int MT, int NT, bool Q8>
-int32_t launch_shrink(precc_ctx* ctx, const AdaptedParams& p, cudaStream_t stream) {
-  const long long tiles = (p.M + 8LL * NT - 1) / (8 * NT);
+int32_t launch_shrink(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
   int ks = 8;                                    // blocks that share the K extent of a row tile
-  while (ks > 1 && (p.K / 64 < ks * SHRINK_WARPS || tiles * ks > 2LL * ctx->sm_count)) ks >>= 1;
+  while (ks > 1 && (p.K / 64 < ks * SHRINK_WARPS || (p.M + 8LL * NT - 1) / (8 * NT) * ks > 2LL * ctx->sm_count)) ks >>= 1;
+  p.tile_rows = 8 * NT;
+  while (p.tile_rows > 1 && (p.M + p.tile_rows / 2 - 1LL) / (p.tile_rows / 2) * ks <= ctx->sm_count) p.tile_rows /= 2;
+  const long long tiles = (p.M + p.tile_rows - 1LL) / p.tile_rows;
   Launch l(dim3((unsigned)(tiles * ks)), SHRINK_THREADS, 0, ks, stream);
   PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_shrink_kernel<MT, NT, Q8>, p));
   return PRECC_OK;
@@ -150,6 +154,69 @@ int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t st
   return PRECC_OK;
 }
 
+template <int NT, int MT, bool Q8>
+int32_t launch_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaStream_t stream) {
+  const int smem = af_smem_bytes(NT, MT, p.agent_id ? p.rank_pad : 0);
+  PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_few_kernel<NT, MT, Q8>, smem));
+  Launch l(dim3((unsigned)((p.N + 16 * MT - 1) / (16 * MT))), AF_THREADS, smem, 1, stream);
+  PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_few_kernel<NT, MT, Q8>, p, (const uint8_t*)W));
+  return PRECC_OK;
+}
+template <bool Q8>
+int32_t run_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaStream_t stream) {
+  static const int force = getenv("AF_MT") ? atoi(getenv("AF_MT")) : 0;
+  const bool wide = force ? force == 2 : p.N > 16 * 4 * ctx->sm_count;
+  if (p.M <= 8) return wide ? launch_few<1, 2, Q8>(ctx, p, W, stream) : launch_few<1, 1, Q8>(ctx, p, W, stream);
+  return wide ? launch_few<2, 2, Q8>(ctx, p, W, stream) : launch_few<2, 1, Q8>(ctx, p, W, stream);
+}
+
+int env_int(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 0; }
+
+template <bool Q8>
+int32_t run_turn(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t stream) {
+  const int nkb = p.K / (Q8 ? 128 : 64);
+  const int* fit = turn_clusters(ctx);
+  const int limit = ctx->max_smem_optin - (p.agent_id ? SHRINK_SMEM : 0);
+  const int groups = (p.N + PT_COLS - 1) / PT_COLS;
+  const int f_tn = env_int("AT_TN"), f_ks = env_int("AT_KS");
+  int best_tn = 0, best_ks = 0, best_st = 0;
+  double best = 1e30;
+  for (int t = (p.M + PT_MAX_TN - 1) / PT_MAX_TN, last = 0; t <= p.M; ++t) {
+    int tn = ((p.M + t - 1) / t + 15) / 16 * 16;
+    if (f_tn) tn = f_tn;
+    if (tn == last) { if (tn == 16) break; else continue; }
+    last = tn;
+    const long long tiles = (p.M + tn - 1) / tn;
+    for (int ks = 1; ks <= GEMM_MAX_KS && nkb >= ks; ++ks) {
+      if (f_ks && ks != f_ks) continue;
+      const int resident = ks == 1 ? ctx->sm_count : fit[ks];
+      if (resident < 1) continue;
+      const long long waves = (groups * tiles + resident - 1) / resident;
+      const int kb = (nkb + ks - 1) / ks;
+      int st = std::min(kb, PT_MAX_STAGES);
+      while (st > 0 && at_smem_bytes(tn, ks, st) > limit) --st;
+      if (st < std::min(kb, 3)) continue;
+      const double cost = waves * (1.5 + kb * (0.37 + 0.00036 * tn) + 0.005 * pt_share(tn, ks) * (ks - 1) + 0.0113 * tn + 0.1 * ks);
+      if (cost < best) { best = cost; best_tn = tn; best_ks = ks; best_st = st; }
+    }
+    if (f_tn || tn == 16) break;
+  }
+  if (best_ks == 0) return fail(ctx, PRECC_ERR_UNSUPPORTED, "no plan");
+  p.BN = best_tn; p.stages = best_st;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < p.BN) p.tmem_cols <<= 1;
+  if (getenv("AT_SHOW")) fprintf(stderr, "turn M %d N %d K %d: tn %d ks %d st %d cost %.2f\n", p.M, p.N, p.K, best_tn, best_ks, best_st, best);
+  const int smem = std::max(PT_MIN_SMEM, at_smem_bytes(p.BN, best_ks, p.stages));
+  CUtensorMap map_x, map_w;
+  int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, p.BN, Q8);
+  if (!rc) rc = map_weights(ctx, &map_w, W, p.N, p.K, PT_COLS, Q8);
+  if (rc) return rc;
+  PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_turn_kernel<Q8>, smem));
+  Launch l(dim3((unsigned)best_ks, (unsigned)groups, (unsigned)((p.M + p.BN - 1) / p.BN)), AT_THREADS, smem, best_ks, stream);
+  PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_turn_kernel<Q8>, map_x, map_w, p));
+  return PRECC_OK;
+}
+
 int32_t check_projection(precc_ctx* ctx, const precc_projection* d, int step) {
   if (!ctx) return PRECC_ERR_INVALID_ARG;
   if (!d) return fail(ctx, PRECC_ERR_INVALID_ARG, "projection descriptor is null");
@@ -191,6 +258,9 @@ int32_t project(precc_ctx* ctx, const precc_projection* d, const void* X, const 
     rc = run_shrink<Q8>(ctx, p, st);
     if (rc) return rc;
   }
+  const int kind = env_int("AP_KIND"), turn_max = env_int("AP_TURN_MAX") ? env_int("AP_TURN_MAX") : 1024;
+  if ((M <= AF_MAX_ROWS && kind == 0) || kind == 1) return run_few<Q8>(ctx, p, W, st);
+  if ((M <= turn_max && kind == 0) || kind == 2) return run_turn<Q8>(ctx, p, W, st);
   return run_pair<Q8>(ctx, p, W, st);
 }
 

@@ -7,6 +7,36 @@
 #include "proj_small.cuh"
 #include "proj_turn.cuh"
 
+namespace precc {
+
+// Clusters of ks blocks of the turn kernel that are resident at once (one block per SM; a cluster lives inside one GPC), for every ks.
+const int* turn_clusters(precc_ctx* ctx) {
+  static int fit_dev[kMaxDevices][GEMM_MAX_KS + 1] = {{0}};       // [.][0] != 0: asked
+  std::lock_guard<std::recursive_mutex> lk(lazy_mu());
+  int* fit = fit_dev[ctx->device % kMaxDevices];
+  if (fit[0]) return fit;
+  auto kern = proj_turn_kernel<false, 1>;
+  for (int ks = 2; ks <= GEMM_MAX_KS; ++ks) {
+    int n = 0;
+    if (raise_smem_limit(ctx, kern, PT_MIN_SMEM) == cudaSuccess) {
+      cudaLaunchConfig_t qc = {};
+      qc.gridDim = dim3(ks, ctx->sm_count, 1); qc.blockDim = dim3(PT_THREADS); qc.dynamicSmemBytes = PT_MIN_SMEM;
+      cudaLaunchAttribute qa[1];
+      qa[0].id = cudaLaunchAttributeClusterDimension;
+      qa[0].val.clusterDim.x = ks; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
+      qc.attrs = qa; qc.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&n, kern, &qc) != cudaSuccess) { cudaGetLastError(); n = 0; }
+    } else {
+      cudaGetLastError();
+    }
+    fit[ks] = n;
+  }
+  fit[0] = 1;
+  return fit;
+}
+
+}  // namespace precc
+
 using namespace precc;
 
 namespace {
@@ -75,32 +105,6 @@ int32_t launch_small(precc_ctx* ctx, const void* X, int M, int K, const void* Wt
 }
 
 int ilog2(int v) { int s = 0; while ((1 << s) < v) ++s; return s; }
-
-// Clusters of ks blocks of the turn kernel that are resident at once (one block per SM; a cluster lives inside one GPC), for every ks.
-const int* turn_clusters(precc_ctx* ctx) {
-  static int fit_dev[kMaxDevices][GEMM_MAX_KS + 1] = {{0}};       // [.][0] != 0: asked
-  std::lock_guard<std::recursive_mutex> lk(lazy_mu());
-  int* fit = fit_dev[ctx->device % kMaxDevices];
-  if (fit[0]) return fit;
-  auto kern = proj_turn_kernel<false, 1>;
-  for (int ks = 2; ks <= GEMM_MAX_KS; ++ks) {
-    int n = 0;
-    if (raise_smem_limit(ctx, kern, PT_MIN_SMEM) == cudaSuccess) {
-      cudaLaunchConfig_t qc = {};
-      qc.gridDim = dim3(ks, ctx->sm_count, 1); qc.blockDim = dim3(PT_THREADS); qc.dynamicSmemBytes = PT_MIN_SMEM;
-      cudaLaunchAttribute qa[1];
-      qa[0].id = cudaLaunchAttributeClusterDimension;
-      qa[0].val.clusterDim.x = ks; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
-      qc.attrs = qa; qc.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&n, kern, &qc) != cudaSuccess) { cudaGetLastError(); n = 0; }
-    } else {
-      cudaGetLastError();
-    }
-    fit[ks] = n;
-  }
-  fit[0] = 1;
-  return fit;
-}
 
 template <int NG>
 int32_t launch_turn(precc_ctx* ctx, const void* X, int M, int K, const void* Wt, int n_out, GemmParams gp, const TurnPlan& tp, cudaStream_t stream) {

@@ -82,6 +82,7 @@ int32_t check_desc(precc_ctx* ctx, const precc_layer_desc* d);
 int32_t check_device(precc_ctx* ctx);        // the context's device is the current one
 int32_t check_cache(precc_ctx* ctx, const precc_layer_desc* d, const precc_cache* c, bool need_base, bool need_lr);
 float softmax_scale_log2(const precc_layer_desc* d);
+const int* turn_clusters(precc_ctx* ctx);    // [ks]: clusters of ks blocks, one block per SM, that are resident at once (ks 2 .. 8)
 
 int32_t make_map(precc_ctx* ctx, CUtensorMap* map, const void* base, int rows, int cols, int box_rows);
 int32_t make_map_w(precc_ctx* ctx, CUtensorMap* map, const void* base, int rows, int K, int box_rows);

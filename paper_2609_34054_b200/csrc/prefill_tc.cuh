@@ -240,11 +240,6 @@ __device__ __forceinline__ void add2(float& lo, float& hi, float b0, float b1) {
 }
 // True in one lane of the (converged) warp, always the same one.  Unlike a lane-id comparison it tells the compiler that the
 // guarded code runs in a single lane, so MMA and TMA operands stay in uniform registers.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t pred;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(pred));
-  return pred != 0;
-}
 
 // WL: the work-list form (helper blocks; a block takes a list of tile pieces).  It is a separate instantiation so that
 // the classic launch carries none of its state through the step loop.
