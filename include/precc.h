@@ -440,7 +440,8 @@ int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, cons
  * X, W and its own agent's A and B alone, also where others hold infinities or NaN.  The order of the sums depends
  * on M, the sizes and the device, not on the other rows' agents.
  * 8 bits: X and W are e4m3, X[m] = x_scale[m] * X_e4m3[m] (as precc_rms_norm leaves it), W_packed and w_scale [n_out] from
- * precc_pack_kmajor_e4m3; A stays bf16, B_packed comes from precc_pack_expand_e4m3.
+ * precc_pack_kmajor_e4m3, A_packed and a_scale [n_agents*rank] from precc_pack_adapter_e4m3, B_packed from
+ * precc_pack_expand_e4m3.
  * Supported: k_dim a multiple of 64 (8 bits: 128), n_out of 8, both up to 2^20; rank 0, 8, 16, 32 or 64; up to 64 agents;
  * M up to 2^26.  M == 0 is a no-op. */
 typedef struct {
@@ -455,14 +456,20 @@ int32_t precc_adapted_project(precc_ctx* ctx, const precc_projection* proj, cons
                               const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream);
 int32_t precc_adapted_project_e4m3(precc_ctx* ctx, const precc_projection* proj, const void* X,
                                    const float* x_scale, int32_t M, const void* W_packed,
-                                   const float* w_scale, const void* A_packed, const void* B_packed,
-                                   const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream);
+                                   const float* w_scale, const void* A_packed, const float* a_scale,
+                                   const void* B_packed, const int32_t* agent_id, void* Y, void* ws,
+                                   size_t ws_bytes, void* stream);
 
 /* Weights in 8 bits.  src bf16 [k_dim][n_cols] -> dst e4m3 [k_dim/128][n_cols][128], scale [n_cols]: the least power of two
  * (2^-100 at least) with which the largest magnitude of the column is at most 448; 1 for a column of zeros.
  * Weights must be finite. */
 int32_t precc_pack_kmajor_e4m3(precc_ctx* ctx, const void* src, int32_t k_dim, int32_t n_cols, void* dst,
                                float* scale, void* stream);
+/* A bf16 [k_dim][rank] of one agent -> its rows of dst e4m3 [k_dim/128][2][n_agents*rank][128] and of scale [n_agents*rank].  A is kept as the
+ * sum of two e4m3 matrices with one power of two per coordinate, the rounded value and what the rounding left: exact where
+ * |A| is at least 2^-9 of the coordinate's largest, off by at most 2^-17 of that below.  A must be finite. */
+int32_t precc_pack_adapter_e4m3(precc_ctx* ctx, const void* A, int32_t k_dim, int32_t rank, int32_t agent,
+                                int32_t n_agents, void* dst, float* scale, void* stream);
 /* B bf16 [rows][n_cols] -> dst = bf16(B / w_scale[column]) (exact for powers of two). */
 int32_t precc_pack_expand_e4m3(precc_ctx* ctx, const void* B, int32_t rows, int32_t n_cols, const float* w_scale,
                                void* dst, void* stream);

@@ -30,7 +30,7 @@ EXPORTS = [
     "precc_prefill_rope_scratch_bytes", "precc_lr_attend_prefill_rope_scratch",
     "precc_prefill_ws_bytes", "precc_lr_attend_prefill_ws",
     "precc_rms_norm", "precc_adapted_ws_bytes", "precc_adapted_project", "precc_adapted_project_e4m3", "precc_pack_kmajor_e4m3",
-    "precc_pack_expand_e4m3",
+    "precc_pack_adapter_e4m3", "precc_pack_expand_e4m3",
 ]
 
 
@@ -128,8 +128,9 @@ def load_library() -> C.CDLL:
     lib.precc_adapted_ws_bytes.argtypes = [pd, i32]
     lib.precc_adapted_ws_bytes.restype = sz
     lib.precc_adapted_project.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
-    lib.precc_adapted_project_e4m3.argtypes = [vp, pd, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.precc_adapted_project_e4m3.argtypes = [vp, pd, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.precc_pack_kmajor_e4m3.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+    lib.precc_pack_adapter_e4m3.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp]
     lib.precc_pack_expand_e4m3.argtypes = [vp, vp, i32, i32, vp, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
@@ -188,8 +189,8 @@ class AdaptedWeights:
     """One projection with its agents' adapters as the kernels take it (see ``Precc.adapted_weights``)."""
 
     def __init__(self, desc: ProjectionDesc, W: torch.Tensor, w_scale: Optional[torch.Tensor], A: Optional[torch.Tensor],
-                 B: Optional[torch.Tensor]):
-        self.desc, self.W, self.w_scale, self.A, self.B = desc, W, w_scale, A, B
+                 B: Optional[torch.Tensor], a_scale: Optional[torch.Tensor] = None):
+        self.desc, self.W, self.w_scale, self.A, self.B, self.a_scale = desc, W, w_scale, A, B, a_scale
 
 
 class Precc:
@@ -415,16 +416,21 @@ class Precc:
         else:
             packed = torch.empty((n, k), dtype=torch.bfloat16, device=W.device)
             self.pack_kmajor(W, packed, 0)
-        A_packed = None
-        if r:
+        A_packed = a_scale = None
+        if r and e4m3:
+            A_packed = torch.empty((k // 128, 2, agents * r, 128), dtype=torch.float8_e4m3fn, device=W.device)
+            a_scale = torch.empty(agents * r, dtype=torch.float32, device=W.device)
+            for a in range(agents):
+                self._check(self.lib.precc_pack_adapter_e4m3(self.h, _ptr(A[a]), k, r, a, agents, _ptr(A_packed), _ptr(a_scale), _stream()),
+                            "precc_pack_adapter_e4m3")
+            B, src = torch.empty_like(B), B
+            self._check(self.lib.precc_pack_expand_e4m3(self.h, _ptr(src), agents * r, n, _ptr(w_scale), _ptr(B), _stream()),
+                        "precc_pack_expand_e4m3")
+        elif r:
             A_packed = torch.empty((agents * r, k), dtype=torch.bfloat16, device=W.device)
             for a in range(agents):
                 self.pack_kmajor(A[a], A_packed, a * r)
-            if e4m3:
-                B, src = torch.empty_like(B), B
-                self._check(self.lib.precc_pack_expand_e4m3(self.h, _ptr(src), agents * r, n, _ptr(w_scale), _ptr(B), _stream()),
-                            "precc_pack_expand_e4m3")
-        return AdaptedWeights(ProjectionDesc(k, n, agents, r, scale), packed, w_scale, A_packed, B if r else None)
+        return AdaptedWeights(ProjectionDesc(k, n, agents, r, scale), packed, w_scale, A_packed, B if r else None, a_scale)
 
     def adapted_workspace(self, weights: AdaptedWeights, max_rows: int) -> Optional[torch.Tensor]:
         """Scratch for calls of up to max_rows rows (None where the projection has no adapters)."""

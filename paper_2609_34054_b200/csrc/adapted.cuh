@@ -1,15 +1,13 @@
 // The projection of a batch whose rows belong to different agents, Y[m] = X[m] W + s (X[m] A_a(m)) B_a(m):  what its kernels share,
 // and the rank-r product T = s X A_a of every row with its own agent's A (bf16, [M][rank, at least 16]).
 //
-// T is small work (2 M K r flops) that the main kernel needs only at its end, so it runs beside it: this kernel lets its
+// T is small work (2 M K r flops) that the main kernel needs only at its end.  For few rows it runs beside it: the shrink kernel lets its
 // dependent start as soon as all its own blocks run - behind its own wait for the kernel ahead, so whatever
 // the dependent reads before ITS wait was complete before either started - and uses little shared memory and few registers, so
-// that a block of the main kernel fits on the same SM.
+// that a block of the main kernel fits on the same SM.  For many rows it is a kernel on the tensor cores of its own (adapted_shrink.cuh).
 // T is rounded to bf16, the operand type of the MMA that takes it: 2^-8 of the adapter's term, which is added to a sum that is
 // rounded to bf16 as a whole.
 #pragma once
-#include <cuda_fp16.h>
-
 #include "norm.cuh"
 #include "tc_common.cuh"
 
@@ -25,7 +23,8 @@ struct AdaptedParams {
   const void* x;                              // [M][K] bf16 or e4m3
   const float* x_scale;                       // 8 bits: [M]
   const float* w_scale;                       // 8 bits: [N]
-  const __nv_bfloat16* A;                     // packed [K/64][n_agents * rank][64]
+  const void* A;                              // packed bf16 [K/64][n_agents * rank][64], or e4m3 [K/128][2: value, rest][n_agents * rank][128]
+  const float* a_scale;                       // 8 bits: [n_agents * rank]
   const __nv_bfloat16* B;                     // [n_agents][rank][N] (8 bits: divided by w_scale)
   __nv_bfloat16* T;                           // [M][rank_pad]
   __nv_bfloat16* y;                           // [M][N]
@@ -35,6 +34,17 @@ struct AdaptedParams {
   uint32_t* status;
 };
 
+// A walk over the slots of a ring: the slot, and the parity of its present round.  (Counted along: a division by the number of slots, which is
+// not known when the kernel is compiled, would cost the issuing warps more than the instructions they issue.)
+struct RingWalk {
+  int s = 0;
+  uint32_t parity = 0;
+  bool filled = false;                        // the first round is over: slots have to be waited for
+  __device__ __forceinline__ void next(int slots) {
+    if (++s == slots) { s = 0; parity ^= 1u; filled = true; }
+  }
+};
+
 // An agent id as the kernels use it: out of range counts as "no adapter" (reported by the shrink kernel).
 __device__ __forceinline__ int agent_of(const AdaptedParams& p, long long row) {
   if (row >= p.M) return -1;
@@ -42,17 +52,29 @@ __device__ __forceinline__ int agent_of(const AdaptedParams& p, long long row) {
   return a < p.n_agents ? a : -1;
 }
 
-// Eight e4m3 values as bf16 (exact).
-__device__ __forceinline__ void e4m3x8_to_bf16(uint32_t lo, uint32_t hi, uint32_t (&o)[4]) {
-  const uint32_t w[2] = {lo, hi};
+// The agents among rows m0 .. m0 + 255 (as far as `rows` of them), one bit each; id[i] is the agent of row 32 i + lane.
+__device__ __forceinline__ unsigned long long agents_of_rows(const AdaptedParams& p, long long m0, int rows, int lane, int (&id)[8]) {
+  unsigned lo = 0, hi = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint16_t two = static_cast<uint16_t>(w[i >> 1] >> (16 * (i & 1)));
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(h) : "h"(two));
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    o[i] = pack_bf16(f.x, f.y);
+  for (int i = 0; i < 8; ++i) {
+    id[i] = 32 * i + lane < rows ? agent_of(p, m0 + 32 * i + lane) : -1;
+    if (id[i] >= 0) { if (id[i] < 32) lo |= 1u << id[i]; else hi |= 1u << (id[i] - 32); }
   }
+  return (static_cast<unsigned long long>(__reduce_or_sync(0xffffffffu, hi)) << 32) | __reduce_or_sync(0xffffffffu, lo);
+}
+
+// D(16x8, fp32) += A(16x32, e4m3, row) * B(32x8, e4m3, col)
+__device__ __forceinline__ void mma_e4m3_16832(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four of the instructions above cover 128 bytes of K: 64 bf16 or 128 e4m3.
+template <bool Q8>
+__device__ __forceinline__ void mma_step(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (Q8) mma_e4m3_16832(d, a, b0, b1);
+  else mma_bf16_16816(d, a, b0, b1);
 }
 
 constexpr int SHRINK_WARPS = 8;
@@ -62,8 +84,10 @@ constexpr int SHRINK_THREADS = SHRINK_WARPS * 32;
 // partial sums meet in shared memory in a fixed order.  The rows are the N axis of mma.sync and the coordinates of the rank its M axis, so a row
 // is computed in its own column of the product and nothing of another agent's adapter reaches it: for every agent among the rows
 // the product is taken with the rows of that agent (the others' columns are zero and dropped).
-// Fragments come straight from global memory, 16 bytes a lane: within 64 values of K a lane of a quad takes two runs of eight, and as A and X agree
-// on which, the order of K inside a step does not matter.
+// Fragments come straight from global memory, 16 bytes a lane: of the 128 bytes of a step a lane of a quad takes pieces t and t + 4, and as A and X
+// agree on which, the order of K inside a step does not matter.
+// 8 bits: A is the sum of two e4m3 matrices with a common scale per coordinate, the value and what its rounding left (see
+// pack_adapter_e4m3_kernel), so that it keeps the bits of bf16; the second is simply more steps of K.
 template <int MT, int NT, bool Q8>
 __global__ void __launch_bounds__(SHRINK_THREADS, 2)
 adapted_shrink_kernel(const AdaptedParams p) {
@@ -86,9 +110,11 @@ adapted_shrink_kernel(const AdaptedParams p) {
   }
   unsigned todo = __ballot_sync(0xffffffffu, id >= 0);
   const unsigned with_adapter = todo;
-  const int nkb = p.K / 64;
-  const int kb0 = (int)((long long)rank_c * nkb / KS), kb1 = (int)((long long)(rank_c + 1) * nkb / KS);
+  constexpr int PARTS = Q8 ? 2 : 1;
+  const int steps = p.K / (Q8 ? 128 : 64) * PARTS;
+  const int v0 = (int)((long long)rank_c * steps / KS), v1 = (int)((long long)(rank_c + 1) * steps / KS);
   const int a_rows = p.n_agents * p.rank;
+  const long long row_bytes = (long long)p.K * (Q8 ? 1 : 2);
 
   while (todo) {
     const int a = __shfl_sync(0xffffffffu, id, __ffs(todo) - 1);
@@ -100,39 +126,24 @@ adapted_shrink_kernel(const AdaptedParams p) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) { acc[m][n][0] = acc[m][n][1] = acc[m][n][2] = acc[m][n][3] = 0.f; }
 #pragma unroll 2
-    for (int kb = kb0 + warp; kb < kb1; kb += SHRINK_WARPS) {
-      // bf16: 16-byte pieces t and t + 4 of the 128; e4m3: 16 values 16 t .. 16 t + 15, i.e. pieces 2 t and 2 t + 1 of A
+    for (int v = v0 + warp; v < v1; v += SHRINK_WARPS) {
       uint4 av[MT][2][2];
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int r = m * 16 + h * 8 + g;
-          const uint4* src = reinterpret_cast<const uint4*>(p.A + ((long long)kb * a_rows + a * p.rank + r) * 64);
+          const uint4* src = static_cast<const uint4*>(p.A) + ((long long)v * a_rows + a * p.rank + r) * 8;      // (step v = value or rest of k-block v / 2)
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-            av[m][h][c] = r < p.rank ? __ldg(src + (Q8 ? 2 * t + c : t + 4 * c)) : make_uint4(0, 0, 0, 0);
+          for (int c = 0; c < 2; ++c) av[m][h][c] = r < p.rank ? __ldg(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
         }
       uint4 xv[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const bool on = (mine >> (n * 8 + g)) & 1u;
-        const long long row = row0 + n * 8 + g;
-        xv[n][0] = xv[n][1] = make_uint4(0, 0, 0, 0);
-        if constexpr (Q8) {
-          if (on) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + row * p.K + (long long)kb * 64) + t);
-            uint32_t lo[4], hi[4];
-            e4m3x8_to_bf16(q.x, q.y, lo);
-            e4m3x8_to_bf16(q.z, q.w, hi);
-            xv[n][0] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            xv[n][1] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          }
-        } else if (on) {
-          const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.x) + row * p.K + (long long)kb * 64);
-          xv[n][0] = __ldg(src + t);
-          xv[n][1] = __ldg(src + t + 4);
-        }
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (row0 + n * 8 + g) * row_bytes + (long long)(v / PARTS) * AP_ROW_BYTES);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) xv[n][c] = on ? __ldg(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c)
@@ -142,8 +153,8 @@ adapted_shrink_kernel(const AdaptedParams p) {
           for (int m = 0; m < MT; ++m) {
             const uint32_t a0[4] = {av[m][0][c].x, av[m][1][c].x, av[m][0][c].y, av[m][1][c].y};
             const uint32_t a1[4] = {av[m][0][c].z, av[m][1][c].z, av[m][0][c].w, av[m][1][c].w};
-            mma_bf16_16816(acc[m][n], a0, xv[n][c].x, xv[n][c].y);
-            mma_bf16_16816(acc[m][n], a1, xv[n][c].z, xv[n][c].w);
+            mma_step<Q8>(acc[m][n], a0, xv[n][c].x, xv[n][c].y);
+            mma_step<Q8>(acc[m][n], a1, xv[n][c].z, xv[n][c].w);
           }
     }
     // a row belongs to one agent: its column goes to its place once
@@ -185,6 +196,7 @@ adapted_shrink_kernel(const AdaptedParams p) {
       asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(u) : "r"(dsmem_addr(local, k)));
       v += u;
     }
+    if constexpr (Q8) { if (c < p.rank) v *= p.a_scale[agent_of(p, row0 + r) * p.rank + c]; }
     p.T[(row0 + r) * p.rank_pad + c] = __float2bfloat16(p.s * v);
   }
   if (KS > 1) {

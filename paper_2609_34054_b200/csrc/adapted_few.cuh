@@ -16,13 +16,6 @@ constexpr int AF_WARPS = 8;
 constexpr int AF_THREADS = AF_WARPS * 32;
 constexpr int AF_MAX_ROWS = 16;
 
-// D(16x8, fp32) += A(16x32, e4m3, row) * B(32x8, e4m3, col)
-__device__ __forceinline__ void mma_e4m3_16832(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 // Weights are read once: past L1.
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   uint4 v;
@@ -117,13 +110,8 @@ adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
           const uint32_t a1[4] = {wv[u][m][0][c].z, wv[u][m][1][c].z, wv[u][m][0][c].w, wv[u][m][1][c].w};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            if constexpr (Q8) {
-              mma_e4m3_16832(acc[m][n], a0, xv[u][n][c].x, xv[u][n][c].y);
-              mma_e4m3_16832(acc[m][n], a1, xv[u][n][c].z, xv[u][n][c].w);
-            } else {
-              mma_bf16_16816(acc[m][n], a0, xv[u][n][c].x, xv[u][n][c].y);
-              mma_bf16_16816(acc[m][n], a1, xv[u][n][c].z, xv[u][n][c].w);
-            }
+            mma_step<Q8>(acc[m][n], a0, xv[u][n][c].x, xv[u][n][c].y);
+            mma_step<Q8>(acc[m][n], a1, xv[u][n][c].z, xv[u][n][c].w);
           }
         }
       fetch(u, kb + (u + U) * AF_WARPS);

@@ -79,29 +79,18 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   const uint32_t tmem_base = *tmem_holder;
   if (!adapters) pdl_launch_dependents();
 
-  // the agents among the 256 rows of a tile, one bit each; `id[i]` is the agent of row 32 i + lane
-  auto agents_of = [&](long long m0, int (&id)[8]) -> unsigned long long {
-    unsigned lo = 0, hi = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      id[i] = agent_of(p, m0 + 32 * i + lane);
-      if (id[i] >= 0) { if (id[i] < 32) lo |= 1u << id[i]; else hi |= 1u << (id[i] - 32); }
-    }
-    return (static_cast<unsigned long long>(__reduce_or_sync(0xffffffffu, hi)) << 32) | __reduce_or_sync(0xffffffffu, lo);
-  };
-
   if (warp == 0) {
     const uint32_t full0_lead = map_to_rank(full0, 0);
-    int it = 0;
+    RingWalk at;
     bool waited = false;
     for (long long t = pair; t < n_tiles; t += n_pairs) {
       const int mt = (int)(t / n_tiles_n) * AP_BM;
       const int m0 = mt + (int)rank * GEMM_BM, n0 = (int)(t % n_tiles_n) * p.BN + (int)rank * half_n;
       int id[8];
-      unsigned long long present = adapters ? agents_of(mt, id) : 0ull;
-      for (int kb = 0; kb < nkb; ++kb, ++it) {
-        const int s = it % p.stages;
-        if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
+      unsigned long long present = adapters ? agents_of_rows(p, mt, AP_BM, lane, id) : 0ull;
+      for (int kb = 0; kb < nkb; ++kb, at.next(p.stages)) {
+        const int s = at.s;
+        if (at.filled) mbar_wait(empty0 + 8 * s, at.parity ^ 1u, p.status);
         const uint32_t sa = smem0 + s * stage_bytes;
         if (elect_one()) {
           if (rank == 0) mbar_expect_tx(full0 + 8 * s, step_tx);
@@ -115,10 +104,10 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         pdl_launch_dependents();
         waited = true;
       }
-      for (; present; present &= present - 1, ++it) {
+      for (; present; present &= present - 1, at.next(p.stages)) {
         const int a = __ffsll(present) - 1;
-        const int s = it % p.stages;
-        if (it >= p.stages) mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
+        const int s = at.s;
+        if (at.filled) mbar_wait(empty0 + 8 * s, at.parity ^ 1u, p.status);
         const uint32_t sa = smem0 + s * stage_bytes;
         if (elect_one()) {
           if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2u * (GEMM_BM + b_boxes * 64) * p.rank_pad * 2);
@@ -137,18 +126,19 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       const uint64_t db0 = umma_desc_sw128(smem0 + AP_A_BYTES);
       const uint64_t dt0 = umma_desc_kmajor(smem0, p.rank_pad * 2);
       const uint64_t de0 = umma_desc_mnmajor(smem0 + AP_A_BYTES, 128, p.rank_pad * 128);
-      int it = 0, i = 0;
+      RingWalk at;
+      int i = 0;
       for (long long t = pair; t < n_tiles; t += n_pairs, ++i) {
         const int buf = i & 1;
         const int mt = (int)(t / n_tiles_n) * AP_BM;
         int id[8];
-        unsigned long long present = adapters ? agents_of(mt, id) : 0ull;
+        unsigned long long present = adapters ? agents_of_rows(p, mt, AP_BM, lane, id) : 0ull;
         const uint32_t d = tmem_base + buf * p.BN;
         if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
-          const int s = it % p.stages;
-          mbar_wait(full0 + 8 * s, (it / p.stages) & 1, p.status);
+        for (int kb = 0; kb < nkb; ++kb, at.next(p.stages)) {
+          const int s = at.s;
+          mbar_wait(full0 + 8 * s, at.parity, p.status);
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
           if (elect_one()) {
             const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
@@ -161,13 +151,13 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
           }
           __syncwarp();
         }
-        for (; present; present &= present - 1, ++it) {
+        for (; present; present &= present - 1, at.next(p.stages)) {
           const int a = __ffsll(present) - 1;
           uint32_t off[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) off[j] = ~__ballot_sync(0xffffffffu, id[j] == a);
-          const int s = it % p.stages;
-          mbar_wait(full0 + 8 * s, (it / p.stages) & 1, p.status);
+          const int s = at.s;
+          mbar_wait(full0 + 8 * s, at.parity, p.status);
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
           if (elect_one()) {
             const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);

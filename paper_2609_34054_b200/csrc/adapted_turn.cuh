@@ -8,7 +8,7 @@
 // of it, and column 8 g + j belongs to column g of the j-th MMA, so that it holds sixteen neighbouring columns of the result.
 // The product of a warp's first group is taken before the sums are there.
 #pragma once
-#include "adapted.cuh"
+#include "adapted_shrink.cuh"
 
 namespace precc {
 
@@ -27,14 +27,6 @@ struct AtTables {
 
 __host__ __device__ constexpr int at_smem_bytes(int tn, int ks, int stages) {
   return pt_data_bytes(tn, ks, stages, 1) + ((int)sizeof(AtTables) + 15) / 16 * 16 + (2 * PT_MAX_STAGES + 4) * 8;
-}
-
-__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n"
-      ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
 
 template <bool Q8>
@@ -101,9 +93,10 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
 
   if (warp == 0) {
-    for (int it = p.stages; it < nkb_s; ++it) {
-      const int s = it % p.stages;
-      mbar_wait(empty0 + 8 * s, ((it / p.stages) - 1) & 1, p.status);
+    RingWalk at;                                         // (the first round was requested above)
+    for (int it = p.stages; it < nkb_s; ++it, at.next(p.stages)) {
+      const int s = at.s;
+      mbar_wait(empty0 + 8 * s, at.parity, p.status);
       const uint32_t st = smem0 + s * stage_bytes;
       if (elect_one()) {
         mbar_expect_tx(full0 + 8 * s, stage_bytes);
@@ -118,9 +111,10 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     const uint32_t idesc = Q8 ? umma_idesc_bf16(TN) & ~((1u << 7) | (1u << 10)) : umma_idesc_bf16(TN);     // (e4m3 is format 0)
     const uint64_t dw0 = umma_desc_sw128(smem0);
     const uint64_t dx0 = umma_desc_sw128(smem0 + PT_W_BYTES);
-    for (int it = 0; it < nkb_s; ++it) {
-      const int s = it % p.stages;
-      mbar_wait(full0 + 8 * s, (it / p.stages) & 1, p.status);
+    RingWalk at;
+    for (int it = 0; it < nkb_s; ++it, at.next(p.stages)) {
+      const int s = at.s;
+      mbar_wait(full0 + 8 * s, at.parity, p.status);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       if (elect_one()) {
         const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);

@@ -1,8 +1,11 @@
 // libprecc: the projection of a batch whose rows carry adapters of their own, in bf16 and in 8 bits, and the packing of 8-bit weights.
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "adapted_few.cuh"
 #include "adapted_pair.cuh"
+#include "adapted_shrink.cuh"
 #include "adapted_turn.cuh"
 #include "api_internal.h"
 
@@ -15,6 +18,12 @@ namespace {
 // column is the least power of two 2^s with max <= 448 * 2^s = 1.75 * 2^(8 + s), read off the bits of the maximum: e4m3 is a
 // floating type, so a power of two costs it no precision, and B / scale is exact in bf16.
 constexpr int PACK8_COLS = 32, PACK8_ROWS = 8;
+
+__device__ __forceinline__ int e4m3_scale_exponent(float top) {
+  const uint32_t b = __float_as_uint(top);
+  const int s = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return top == 0.f || (b >> 23) == 255u ? 0 : max(s, -100);
+}
 
 __global__ void __launch_bounds__(PACK8_COLS * PACK8_ROWS)
 pack_kmajor_e4m3_kernel(const __nv_bfloat16* __restrict__ src, int K, int N, uint8_t* __restrict__ dst, float* __restrict__ scale) {
@@ -29,10 +38,7 @@ pack_kmajor_e4m3_kernel(const __nv_bfloat16* __restrict__ src, int K, int N, uin
   __syncthreads();
   if (ty == 0) {
     for (int i = 1; i < PACK8_ROWS; ++i) top = fmaxf(top, top_s[i][tx]);
-    const uint32_t b = __float_as_uint(top);
-    int s = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
-    if (top == 0.f || (b >> 23) == 255u) s = 0;
-    s = max(s, -100);
+    const int s = e4m3_scale_exponent(top);
     inv_s[tx] = __uint_as_float((uint32_t)(127 - s) << 23);
     if (c < N) scale[c] = __uint_as_float((uint32_t)(127 + s) << 23);
   }
@@ -54,6 +60,35 @@ __global__ void pack_expand_e4m3_kernel(const __nv_bfloat16* __restrict__ B, lon
                                         __nv_bfloat16* __restrict__ dst) {
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x)
     dst[i] = __float2bfloat16(__fdiv_rn(__bfloat162float(B[i]), scale[i % N]));
+}
+
+// A of one agent, [K][rank] -> two e4m3 matrices with one power of two per coordinate: hi = e4m3(a / scale) and lo = e4m3(a / scale - hi).  bf16 has eight
+// significant bits and e4m3 four, so hi + lo is a / scale exactly where that is at
+// least 1/4 (2^-9 of the coordinate's largest value), and off by at most half of the least step 2^-9 (2^-17 of the largest) below.
+// dst [K/128][2][n_agents * rank][128].
+__global__ void __launch_bounds__(256)
+pack_adapter_e4m3_kernel(const __nv_bfloat16* __restrict__ src, int K, int rank, int agent, int rows, uint8_t* __restrict__ dst, float* __restrict__ scale) {
+  __shared__ float top_s[8];
+  const int c = blockIdx.x;                                          // the coordinate
+  float top = 0.f;
+  for (int k = threadIdx.x; k < K; k += 256) top = fmaxf(top, fabsf(__bfloat162float(src[(size_t)k * rank + c])));
+  for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+  if ((threadIdx.x & 31) == 0) top_s[threadIdx.x / 32] = top;
+  __syncthreads();
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, top_s[i]);
+  const int s = e4m3_scale_exponent(top);
+  if (threadIdx.x == 0) scale[agent * rank + c] = __uint_as_float((uint32_t)(127 + s) << 23);
+  const float inv = __uint_as_float((uint32_t)(127 - s) << 23);
+  for (int k = threadIdx.x; k < K; k += 256) {
+    const float v = __bfloat162float(src[(size_t)k * rank + c]) * inv;
+    const uint32_t hi = pack_e4m3x4(v, 0.f, 0.f, 0.f) & 0xffu;
+    uint32_t h2;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(h2) : "h"((uint16_t)hi));
+    const float rest = v - __half2float(__ushort_as_half((uint16_t)h2));
+    uint8_t* at = dst + ((size_t)(k / 128) * 2 * rows + agent * rank + c) * 128 + k % 128;
+    at[0] = (uint8_t)hi;
+    at[(size_t)rows * 128] = (uint8_t)pack_e4m3x4(rest, 0.f, 0.f, 0.f);
+  }
 }
 
 // ------------------------------------------------------------------------------------------ tensor maps
@@ -109,8 +144,27 @@ int32_t launch_shrink(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
   PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_shrink_kernel<MT, NT, Q8>, p));
   return PRECC_OK;
 }
+int env_int(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 0; }
+
+template <bool Q8>
+int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
+  const int rounds = (p.M + ctx->sm_count * 256 - 1) / (ctx->sm_count * 256);
+  p.BN = ((p.M + ctx->sm_count * rounds - 1) / (ctx->sm_count * rounds) + 15) / 16 * 16;
+  const int ring = ctx->max_smem_optin - 4096, smem = ring + 1024;
+  CUtensorMap map_x, map_a;
+  int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, p.BN, Q8);
+  if (!rc) rc = map_weights(ctx, &map_a, p.A, p.n_agents * p.rank * (Q8 ? 2 : 1), p.K, p.rank, Q8);
+  if (rc) return rc;
+  PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_shrink_tc_kernel<Q8>, smem));
+  Launch l(dim3((unsigned)((p.M + p.BN - 1) / p.BN)), AS_THREADS, smem, 1, stream);
+  PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_shrink_tc_kernel<Q8>, map_x, map_a, p, ring));
+  return PRECC_OK;
+}
+
 template <bool Q8>
 int32_t run_shrink(precc_ctx* ctx, const AdaptedParams& p, cudaStream_t stream) {
+  const int tc = env_int("AS_TC");
+  if (tc ? p.M >= tc : p.M >= 2048) return launch_shrink_tc<Q8>(ctx, p, stream);
   const bool few = p.M <= 64;
   switch (p.rank_pad) {
     case 16: return few ? launch_shrink<1, 1, Q8>(ctx, p, stream) : launch_shrink<1, 4, Q8>(ctx, p, stream);
@@ -170,8 +224,6 @@ int32_t run_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaStrea
   return wide ? launch_few<2, 2, Q8>(ctx, p, W, stream) : launch_few<2, 1, Q8>(ctx, p, W, stream);
 }
 
-int env_int(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 0; }
-
 template <bool Q8>
 int32_t run_turn(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t stream) {
   const int nkb = p.K / (Q8 ? 128 : 64);
@@ -230,7 +282,7 @@ int32_t check_projection(precc_ctx* ctx, const precc_projection* d, int step) {
 
 template <bool Q8>
 int32_t project(precc_ctx* ctx, const precc_projection* d, const void* X, const float* x_scale, int32_t M, const void* W, const float* w_scale,
-                const void* A, const void* B, const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream) {
+                const void* A, const float* a_scale, const void* B, const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream) {
   int32_t rc = check_projection(ctx, d, Q8 ? 128 : 64);
   if (rc) return rc;
   if (M < 0) return fail(ctx, PRECC_ERR_INVALID_ARG, "M < 0");
@@ -238,10 +290,10 @@ int32_t project(precc_ctx* ctx, const precc_projection* d, const void* X, const 
   if (M == 0) return PRECC_OK;
   if (!X || !W || !Y || (Q8 && (!x_scale || !w_scale))) return fail(ctx, PRECC_ERR_INVALID_ARG, "X / W / Y or a scale is null");
   const bool adapters = agent_id && d->rank > 0;
-  if (adapters && (!A || !B)) return fail(ctx, PRECC_ERR_INVALID_ARG, "A or B is null");
+  if (adapters && (!A || !B || (Q8 && !a_scale))) return fail(ctx, PRECC_ERR_INVALID_ARG, "A, its scales or B is null");
   if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(A) || !aligned16(B) || !aligned16(w_scale) || (reinterpret_cast<uintptr_t>(x_scale) & 3u) ||
-      (reinterpret_cast<uintptr_t>(agent_id) & 3u))
-    return fail(ctx, PRECC_ERR_MISALIGNED, "X / W / Y / A / B / w_scale not 16-byte aligned (x_scale, agent_id: 4)");
+      (reinterpret_cast<uintptr_t>(a_scale) & 3u) || (reinterpret_cast<uintptr_t>(agent_id) & 3u))
+    return fail(ctx, PRECC_ERR_MISALIGNED, "X / W / Y / A / B / w_scale not 16-byte aligned (x_scale, a_scale, agent_id: 4)");
   AdaptedParams p = {};
   p.M = M; p.N = d->n_out; p.K = d->k_dim; p.rank = d->rank; p.rank_pad = std::max(16, d->rank); p.n_agents = d->n_agents;
   p.x = X; p.x_scale = x_scale; p.w_scale = w_scale; p.y = (__nv_bfloat16*)Y; p.s = d->lora_scale; p.status = ctx->status;
@@ -249,7 +301,7 @@ int32_t project(precc_ctx* ctx, const precc_projection* d, const void* X, const 
     const size_t need = precc_adapted_ws_bytes(d, M);
     if (!ws || ws_bytes < need) return fail(ctx, PRECC_ERR_WORKSPACE, "workspace: need %zu bytes, got %zu", need, ws ? ws_bytes : (size_t)0);
     if (reinterpret_cast<uintptr_t>(ws) & 127u) return fail(ctx, PRECC_ERR_MISALIGNED, "workspace not 128-byte aligned");
-    p.agent_id = agent_id; p.A = (const __nv_bfloat16*)A; p.B = (const __nv_bfloat16*)B; p.T = (__nv_bfloat16*)ws;
+    p.agent_id = agent_id; p.A = A; p.a_scale = a_scale; p.B = (const __nv_bfloat16*)B; p.T = (__nv_bfloat16*)ws;
   }
   rc = check_device(ctx);
   if (rc) return rc;
@@ -282,6 +334,20 @@ int32_t precc_pack_kmajor_e4m3(precc_ctx* ctx, const void* src, int32_t k_dim, i
   return PRECC_OK;
 }
 
+int32_t precc_pack_adapter_e4m3(precc_ctx* ctx, const void* A, int32_t k_dim, int32_t rank, int32_t agent, int32_t n_agents, void* dst, float* scale,
+                                void* stream) {
+  if (!ctx) return PRECC_ERR_INVALID_ARG;
+  if (!A || !dst || !scale || k_dim <= 0 || agent < 0 || agent >= n_agents) return fail(ctx, PRECC_ERR_INVALID_ARG, "pack_adapter_e4m3: bad arguments");
+  if (k_dim % 128 || !rank_ok(rank) || n_agents > AP_MAX_AGENTS) return fail(ctx, PRECC_ERR_UNSUPPORTED, "pack_adapter_e4m3: k_dim, rank or n_agents outside the supported set");
+  if ((reinterpret_cast<uintptr_t>(A) & 1u) || !aligned16(dst) || (reinterpret_cast<uintptr_t>(scale) & 3u))
+    return fail(ctx, PRECC_ERR_MISALIGNED, "pack_adapter_e4m3: dst not 16-byte aligned (A: 2, scale: 4)");
+  const int32_t rc = check_device(ctx);
+  if (rc) return rc;
+  pack_adapter_e4m3_kernel<<<rank, 256, 0, (cudaStream_t)stream>>>((const __nv_bfloat16*)A, k_dim, rank, agent, n_agents * rank, (uint8_t*)dst, scale);
+  PRECC_CUDA(ctx, cudaGetLastError());
+  return PRECC_OK;
+}
+
 int32_t precc_pack_expand_e4m3(precc_ctx* ctx, const void* B, int32_t rows, int32_t n_cols, const float* w_scale, void* dst, void* stream) {
   if (!ctx) return PRECC_ERR_INVALID_ARG;
   if (!B || !dst || !w_scale || rows <= 0 || n_cols <= 0) return fail(ctx, PRECC_ERR_INVALID_ARG, "pack_expand_e4m3: bad arguments");
@@ -303,13 +369,13 @@ size_t precc_adapted_ws_bytes(const precc_projection* proj, int32_t M) {
 
 int32_t precc_adapted_project(precc_ctx* ctx, const precc_projection* proj, const void* X, int32_t M, const void* W_packed, const void* A_packed,
                               const void* B, const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream) {
-  return project<false>(ctx, proj, X, nullptr, M, W_packed, nullptr, A_packed, B, agent_id, Y, ws, ws_bytes, stream);
+  return project<false>(ctx, proj, X, nullptr, M, W_packed, nullptr, A_packed, nullptr, B, agent_id, Y, ws, ws_bytes, stream);
 }
 
 int32_t precc_adapted_project_e4m3(precc_ctx* ctx, const precc_projection* proj, const void* X, const float* x_scale, int32_t M,
-                                   const void* W_packed, const float* w_scale, const void* A_packed, const void* B_packed,
+                                   const void* W_packed, const float* w_scale, const void* A_packed, const float* a_scale, const void* B_packed,
                                    const int32_t* agent_id, void* Y, void* ws, size_t ws_bytes, void* stream) {
-  return project<true>(ctx, proj, X, x_scale, M, W_packed, w_scale, A_packed, B_packed, agent_id, Y, ws, ws_bytes, stream);
+  return project<true>(ctx, proj, X, x_scale, M, W_packed, w_scale, A_packed, a_scale, B_packed, agent_id, Y, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -22,7 +22,7 @@ namespace {
 
 PyObject* g_error = nullptr;   // binding.PreccError
 PyObject* g_cache = nullptr;   // binding.Cache
-PyObject *s_desc, *s_k_base, *s_v_base, *s_lr_k, *s_lr_v, *s_n_blocks, *s_W, *s_A, *s_B, *s_w_scale;
+PyObject *s_desc, *s_k_base, *s_v_base, *s_lr_k, *s_lr_v, *s_n_blocks, *s_W, *s_A, *s_B, *s_w_scale, *s_a_scale;
 
 // One call's arguments, taken in order; the first problem sets the Python error and makes the rest no-ops.
 struct Args {
@@ -461,13 +461,15 @@ NATIVE(adapted_project) {
   const at::Tensor* wst = a.tensor();
   const Args::Buffer ws = a.buffer(wst);
   void* W = a.member_sized(w, s_W, "weights.W", Q8 ? at::kFloat8_e4m3fn : at::kBFloat16, (int64_t)d.k_dim * d.n_out, true);
-  void* A = a.member_sized(w, s_A, "weights.A", at::kBFloat16, low * d.k_dim, low > 0);
+  void* A = Q8 ? a.member_sized(w, s_A, "weights.A", at::kFloat8_e4m3fn, 2 * low * d.k_dim, low > 0)
+               : a.member_sized(w, s_A, "weights.A", at::kBFloat16, low * d.k_dim, low > 0);
+  float* as = Q8 ? static_cast<float*>(a.member_sized(w, s_a_scale, "weights.a_scale", at::kFloat, low, low > 0)) : nullptr;
   void* B = a.member_sized(w, s_B, "weights.B", at::kBFloat16, low * d.n_out, low > 0);
   float* wsc = Q8 ? static_cast<float*>(a.member_sized(w, s_w_scale, "weights.w_scale", at::kFloat, d.n_out, true)) : nullptr;
   if (wst && a.ok && wst->get_device() != a.device) a.bad("workspace is on another device than the tensors before it");
   if (!a.on_current_device()) return nullptr;
   return finish(ctx, Q8 ? "precc_adapted_project_e4m3" : "precc_adapted_project", [&](void* st) {
-    if (Q8) return precc_adapted_project_e4m3(ctx, &d, x.p, xs, (int32_t)x.rows, W, wsc, A, B, agent, out, ws.p, ws.bytes, st);
+    if (Q8) return precc_adapted_project_e4m3(ctx, &d, x.p, xs, (int32_t)x.rows, W, wsc, A, as, B, agent, out, ws.p, ws.bytes, st);
     return precc_adapted_project(ctx, &d, x.p, (int32_t)x.rows, W, A, B, agent, out, ws.p, ws.bytes, st); });
 }
 
@@ -525,6 +527,7 @@ PyMODINIT_FUNC PyInit__native() {
   s_A = PyUnicode_InternFromString("A");
   s_B = PyUnicode_InternFromString("B");
   s_w_scale = PyUnicode_InternFromString("w_scale");
+  s_a_scale = PyUnicode_InternFromString("a_scale");
   Py_INCREF(PyExc_RuntimeError);
   g_error = PyExc_RuntimeError;
   return PyModule_Create(&module_def);

@@ -49,8 +49,9 @@ def _quantised(w):
     return (w.double() / s).to(E4M3), s
 
 
-def _reference(x, w, A, B, ids, scale):
-    """Y in 64 bits, and the bound on what the kernels may be off: x, w in double."""
+def _reference(x, w, A, B, ids, scale, e4m3=False):
+    """Y in 64 bits, and the bound on what the kernels may be off: x, w in double.  In 8 bits A is the sum of two e4m3 values, off by at most
+    2^-17 of the coordinate's largest."""
     k = x.shape[1]
     y = x @ w
     # sums of K products in fp32, at most 2^-23 of the magnitudes a step (tensor cores may truncate); T: one rounding to bf16 (2^-8)
@@ -62,7 +63,8 @@ def _reference(x, w, A, B, ids, scale):
                 Aa, Ba = A[a].double(), B[a].double()
                 t = x[rows] @ Aa
                 y[rows] += scale * t @ Ba
-                off[rows] += abs(scale) * ((2.0**-8 * t.abs() + (k + 64) * 2.0**-23 * (x[rows].abs() @ Aa.abs())) @ Ba.abs())
+                a_off = 2.0**-17 * Aa.abs().amax(0) * x[rows].abs().sum(1, keepdim=True) if e4m3 else 0
+                off[rows] += abs(scale) * ((2.0**-8 * t.abs() + (k + 64) * 2.0**-23 * (x[rows].abs() @ Aa.abs()) + a_off) @ Ba.abs())
     return y, off + 2.0**-8 * y.abs() + 1e-30
 
 
@@ -84,7 +86,7 @@ def _run(px, rows, k, n, r, agents, mix, e4m3, scale=1.5, seed=0, ids=None, chec
         px.adapted_project(wt, x, out[:rows], ids, ws)
         xd, wd = x.double(), w.double()
     assert torch.isnan(out[rows:]).all()    # rows behind the last one stay
-    y, bound = _reference(xd, wd, A, B, ids, scale)
+    y, bound = _reference(xd, wd, A, B, ids, scale, e4m3)
     if check:
         err = (out[:rows].double() - y).abs()
         assert torch.isfinite(out[:rows]).all()
@@ -97,7 +99,7 @@ def _run(px, rows, k, n, r, agents, mix, e4m3, scale=1.5, seed=0, ids=None, chec
 
 SIZES = [(1, 64, 8), (1, 2048, 2048), (2, 128, 24), (7, 1024, 1000), (16, 3584, 3584), (17, 256, 136), (40, 4096, 2304), (64, 512, 64), (65, 1024, 520),
          (127, 192, 264), (128, 256, 256), (129, 2048, 128), (200, 3584, 1280), (256, 1024, 1024), (257, 640, 200), (333, 1024, 1000),
-         (511, 128, 2048), (700, 4096, 512), (1500, 256, 4096), (3001, 320, 328)]
+         (511, 128, 2048), (700, 4096, 512), (1500, 256, 4096), (3001, 320, 328), (9000, 128, 136)]
 
 
 @pytest.mark.parametrize("rank", [0, 8, 16, 32, 64])
@@ -121,7 +123,7 @@ def test_agents(px, rows, mix, e4m3):
 
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("rank", [8, 64])
-@pytest.mark.parametrize("rows", [3, 61, 256, 900])
+@pytest.mark.parametrize("rows", [3, 61, 256, 900, 2500, 40000])
 def test_64_agents(px, rows, rank, e4m3):
     _run(px, rows, 512, 328, rank, 64, "rows", e4m3)
 
@@ -133,7 +135,7 @@ def test_the_largest_width_and_depth(px, rows):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
-@pytest.mark.parametrize("rows", [1, 6, 24, 70, 150, 400, 1300])
+@pytest.mark.parametrize("rows", [1, 6, 24, 70, 150, 400, 1300, 2600])
 def test_other_adapters_and_rows_do_not_reach_a_row(px, rows, e4m3):
     """Bit for bit the same whatever the other agents' adapters and the other rows hold, infinities and NaN among them."""
     k, n, r, agents = 512, 264, 16, 6
@@ -173,7 +175,7 @@ def test_other_adapters_and_rows_do_not_reach_a_row(px, rows, e4m3):
     assert not torch.isfinite(got[0]).any() and torch.equal(got[~mine], want[~mine])
 
 
-@pytest.mark.parametrize("rows", [2, 30, 100, 600])
+@pytest.mark.parametrize("rows", [2, 30, 100, 600, 2300])
 def test_bad_agent_ids_are_reported_and_skipped(px, rows):
     ids = _ids(rows, 4, "rows")
     good = ids.clone()
@@ -211,6 +213,21 @@ def test_packed_8_bit_weights(px, k, n):
     px._check(px.lib.precc_pack_expand_e4m3(px.h, B.data_ptr(), 6, n, scale.data_ptr(), dst.data_ptr(), st), "pack")
     keep = [i for i in range(n) if i not in (3, 4)]          # (B / 2^-100 and B / 2^120 leave bf16's range)
     assert torch.equal(dst.double()[:, keep], (B.double() / s)[:, keep])
+
+
+@pytest.mark.parametrize("k,r", [(128, 8), (384, 64), (4096, 16)])
+def test_packed_8_bit_adapters(px, k, r):
+    """Value and rest sum up to A: exactly down to 2^-9 of a coordinate's largest value, within 2^-17 of that below."""
+    A = (I.normal_bf16((3, k, r), 1.0, 1, "adapted.packA").double() * torch.exp2(torch.randint(-24, 1, (3, k, r), generator=torch.Generator().manual_seed(3)))).to(torch.bfloat16).cuda()
+    A[1, :, 0] = 0
+    wt = px.adapted_weights(torch.zeros((k, 8), dtype=torch.bfloat16, device="cuda"), A, torch.zeros((3, r, 8), dtype=torch.bfloat16, device="cuda"), 1.0, e4m3=True)
+    parts = wt.A.view(k // 128, 2, 3, r, 128).double().permute(1, 2, 0, 4, 3).reshape(2, 3, k, r)
+    got = parts.sum(0) * wt.a_scale.double().view(3, 1, r)
+    top = A.double().abs().amax(1, keepdim=True)
+    s = torch.where(top > 0, torch.exp2(torch.ceil(torch.log2(top / 448))), torch.ones_like(top))
+    assert torch.equal(wt.a_scale.double().view(3, 1, r), s)
+    err = (got - A.double()).abs()
+    assert (err <= 2.0**-17 * top).all() and (err[A.double().abs() >= 2.0**-9 * top] == 0).all()
 
 
 @pytest.mark.parametrize("rows", [1, 9, 64, 300, 1100])
