@@ -36,6 +36,8 @@ struct AdaptedParams {
 
 // A walk over the slots of a ring: the slot, and the parity of its present round.  (Counted along: a division by the number of slots, which is
 // not known when the kernel is compiled, would cost the issuing warps more than the instructions they issue.)
+// The loops that issue copies and MMAs run in one elected thread from end to end.  With an election in every step, and the whole warp waiting on
+// the barriers, a step of four MMAs took 364 .. 388 cycles; so it takes 263 up to 128 columns, and what the MMAs take beyond.
 struct RingWalk {
   int s = 0;
   uint32_t parity = 0;
@@ -43,22 +45,36 @@ struct RingWalk {
   __device__ __forceinline__ void next(int slots) {
     if (++s == slots) { s = 0; parity ^= 1u; filled = true; }
   }
+  __device__ __forceinline__ void skip(int n, int slots) {
+    const int to = s + n, rounds = to / slots;
+    s = to - rounds * slots;
+    parity ^= rounds & 1;
+    filled |= rounds > 0;
+  }
 };
 
 // An agent id as the kernels use it: out of range counts as "no adapter" (reported by the shrink kernel).
 __device__ __forceinline__ int agent_of(const AdaptedParams& p, long long row) {
   if (row >= p.M) return -1;
   const int a = p.agent_id[row];
-  return a < p.n_agents ? a : -1;
+  return a >= 0 && a < p.n_agents ? a : -1;
 }
 
-// The agents among rows m0 .. m0 + 255 (as far as `rows` of them), one bit each; id[i] is the agent of row 32 i + lane.
-__device__ __forceinline__ unsigned long long agents_of_rows(const AdaptedParams& p, long long m0, int rows, int lane, int (&id)[8]) {
+// The agents of the 256 rows from m0 on, as far as `rows` of them (id[i]: row 32 i + lane).  Asked for at once and looked at later: eight loads
+// behind conditions of their own wait for one another, 4 us a tile.
+__device__ __forceinline__ void load_agents(const AdaptedParams& p, long long m0, int lane, int (&id)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) id[i] = __ldg(p.agent_id + min(m0 + 32 * i + lane, (long long)p.M - 1));
+}
+// One bit for each agent among them; ids out of range, and rows past M or `rows`, become -1.
+__device__ __forceinline__ unsigned long long agents_present(const AdaptedParams& p, long long m0, int rows, int lane, int (&id)[8]) {
   unsigned lo = 0, hi = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    id[i] = 32 * i + lane < rows ? agent_of(p, m0 + 32 * i + lane) : -1;
-    if (id[i] >= 0) { if (id[i] < 32) lo |= 1u << id[i]; else hi |= 1u << (id[i] - 32); }
+    const bool on = 32 * i + lane < rows && m0 + 32 * i + lane < p.M && id[i] >= 0 && id[i] < p.n_agents;
+    if (!on) id[i] = -1;
+    lo |= on && id[i] < 32 ? 1u << (id[i] & 31) : 0u;
+    hi |= on && id[i] >= 32 ? 1u << (id[i] & 31) : 0u;
   }
   return (static_cast<unsigned long long>(__reduce_or_sync(0xffffffffu, hi)) << 32) | __reduce_or_sync(0xffffffffu, lo);
 }

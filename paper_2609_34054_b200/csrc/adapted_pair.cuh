@@ -10,7 +10,8 @@
 
 namespace precc {
 
-constexpr int AP_THREADS = 192;                       // producer, MMA issuer, four epilogue warps
+constexpr int AP_EPI_WARPS = 4;
+constexpr int AP_THREADS = (2 + AP_EPI_WARPS) * 32;   // producer, MMA issuer, epilogue warps
 constexpr int AP_BM = 2 * GEMM_BM;
 constexpr int AP_A_BYTES = GEMM_BM * AP_ROW_BYTES;
 
@@ -61,6 +62,9 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   const bool adapters = p.agent_id != nullptr;
 
   if (threadIdx.x == 0) {
+    prefetch_map(&map_x);
+    prefetch_map(&map_w);
+    if (adapters) { prefetch_map(&map_t); prefetch_map(&map_b); }
     for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     mbar_init(acc_full, 1); mbar_init(acc_full + 8, 1);
     mbar_init(acc_empty, 8); mbar_init(acc_empty + 8, 8);
@@ -87,36 +91,39 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       const int mt = (int)(t / n_tiles_n) * AP_BM;
       const int m0 = mt + (int)rank * GEMM_BM, n0 = (int)(t % n_tiles_n) * p.BN + (int)rank * half_n;
       int id[8];
-      unsigned long long present = adapters ? agents_of_rows(p, mt, AP_BM, lane, id) : 0ull;
-      for (int kb = 0; kb < nkb; ++kb, at.next(p.stages)) {
-        const int s = at.s;
-        if (at.filled) mbar_wait(empty0 + 8 * s, at.parity ^ 1u, p.status);
-        const uint32_t sa = smem0 + s * stage_bytes;
-        if (elect_one()) {
-          if (rank == 0) mbar_expect_tx(full0 + 8 * s, step_tx);
-          tma_pair_load_2d(sa, &map_x, kb * (Q8 ? 128 : 64), m0, full0_lead + 8 * s);
-          tma_pair_load_3d(sa + AP_A_BYTES, &map_w, 0, n0, kb, full0_lead + 8 * s);
+      if (adapters) load_agents(p, mt, lane, id);
+      if (elect_one()) {
+        RingWalk w = at;
+        for (int kb = 0; kb < nkb; ++kb, w.next(p.stages)) {
+          if (w.filled) mbar_wait(empty0 + 8 * w.s, w.parity ^ 1u, p.status);
+          const uint32_t sa = smem0 + w.s * stage_bytes, bar = full0_lead + 8 * w.s;
+          if (rank == 0) mbar_expect_tx(full0 + 8 * w.s, step_tx);
+          tma_pair_load_3d(sa, &map_x, 0, m0, kb, bar);
+          tma_pair_load_3d(sa + AP_A_BYTES, &map_w, 0, n0, kb, bar);
         }
-        __syncwarp();
       }
-      if (adapters && !waited) {       // T is complete; also with no adapter in this tile, so that this grid ends after the shrink kernel
+      __syncwarp();
+      at.skip(nkb, p.stages);
+      if (!adapters) continue;
+      if (!waited) {                   // T is complete; also with no adapter in this tile, so that this grid ends after the shrink kernel
         pdl_wait();
         pdl_launch_dependents();
         waited = true;
       }
-      for (; present; present &= present - 1, at.next(p.stages)) {
-        const int a = __ffsll(present) - 1;
-        const int s = at.s;
-        if (at.filled) mbar_wait(empty0 + 8 * s, at.parity ^ 1u, p.status);
-        const uint32_t sa = smem0 + s * stage_bytes;
-        if (elect_one()) {
-          if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2u * (GEMM_BM + b_boxes * 64) * p.rank_pad * 2);
-          tma_pair_load_2d(sa, &map_t, 0, m0, full0_lead + 8 * s);
+      const unsigned long long present = agents_present(p, mt, AP_BM, lane, id);
+      if (elect_one()) {
+        RingWalk w = at;
+        for (unsigned long long left = present; left; left &= left - 1, w.next(p.stages)) {
+          if (w.filled) mbar_wait(empty0 + 8 * w.s, w.parity ^ 1u, p.status);
+          const uint32_t sa = smem0 + w.s * stage_bytes, bar = full0_lead + 8 * w.s;
+          if (rank == 0) mbar_expect_tx(full0 + 8 * w.s, 2u * (GEMM_BM + b_boxes * 64) * p.rank_pad * 2);
+          tma_pair_load_2d(sa, &map_t, 0, m0, bar);
           for (int j = 0; j < b_boxes; ++j)
-            tma_pair_load_3d(sa + AP_A_BYTES + j * p.rank_pad * 128, &map_b, n0 + 64 * j, 0, a, full0_lead + 8 * s);
+            tma_pair_load_3d(sa + AP_A_BYTES + j * p.rank_pad * 128, &map_b, n0 + 64 * j, 0, __ffsll(left) - 1, bar);
         }
-        __syncwarp();
       }
+      __syncwarp();
+      at.skip(__popcll(present), p.stages);
     }
   } else if (warp == 1) {
     if (rank == 0) {
@@ -132,38 +139,38 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         const int buf = i & 1;
         const int mt = (int)(t / n_tiles_n) * AP_BM;
         int id[8];
-        unsigned long long present = adapters ? agents_of_rows(p, mt, AP_BM, lane, id) : 0ull;
+        if (adapters) load_agents(p, mt, lane, id);
         const uint32_t d = tmem_base + buf * p.BN;
-        if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
-        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-        for (int kb = 0; kb < nkb; ++kb, at.next(p.stages)) {
-          const int s = at.s;
-          mbar_wait(full0 + 8 * s, at.parity, p.status);
-          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-          if (elect_one()) {
-            const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
+        if (elect_one()) {
+          if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
+          RingWalk w = at;
+          for (int kb = 0; kb < nkb; ++kb, w.next(p.stages)) {
+            mbar_wait(full0 + 8 * w.s, w.parity, p.status);
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+            const uint64_t so = (uint64_t)((w.s * stage_bytes) >> 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {             // 32 bytes of K a step: 16 bf16 or 32 e4m3
               if constexpr (Q8) umma_pair_e4m3(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
               else umma_pair_bf16(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
             }
-            umma_pair_commit_both(empty0 + 8 * s);
+            umma_pair_commit_both(empty0 + 8 * w.s);
           }
-          __syncwarp();
         }
-        for (; present; present &= present - 1, at.next(p.stages)) {
-          const int a = __ffsll(present) - 1;
+        __syncwarp();
+        at.skip(nkb, p.stages);
+        const unsigned long long present = adapters ? agents_present(p, mt, AP_BM, lane, id) : 0ull;
+        for (unsigned long long left = present; left; left &= left - 1, at.next(p.stages)) {
+          const int a = __ffsll(left) - 1;
           uint32_t off[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) off[j] = ~__ballot_sync(0xffffffffu, id[j] == a);
-          const int s = at.s;
-          mbar_wait(full0 + 8 * s, at.parity, p.status);
-          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
           if (elect_one()) {
-            const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
+            mbar_wait(full0 + 8 * at.s, at.parity, p.status);
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+            const uint64_t so = (uint64_t)((at.s * stage_bytes) >> 4);
             for (int k = 0; k < p.rank_pad / 16; ++k)
               umma_pair_bf16_lanes(d, dt0 + so + 2 * k, de0 + so + 128 * k, idesc_b, off);
-            umma_pair_commit_both(empty0 + 8 * s);
+            umma_pair_commit_both(empty0 + 8 * at.s);
           }
           __syncwarp();
         }

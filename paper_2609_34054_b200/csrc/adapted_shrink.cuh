@@ -1,6 +1,7 @@
 // T = s X A_a of every row with its own agent's A, for many rows: one pass over X on tcgen05.
 //
-// HBM-bound at M x K values of X.  A block takes TN rows (as many as spread them over all SMs) over the whole K extent.  The coordinates of the rank are
+// HBM-bound at M x K values of X.  A block takes TN rows (as many as spread them over all SMs) over the whole K extent, or, where that would leave SMs
+// idle, the blocks of a cluster share the K extent and add their sums in rank order.  The coordinates of the rank are
 // the M axis of the MMA, 128 lanes that hold the coordinates of up to 128 / r agents, and the rows of X its N axis: a row is computed with every
 // agent among the rows of its block, and the lanes of its own agent are the ones that are written.  Rows of one request follow one
 // another, so a block mostly sees one or two agents.  Where it sees more than 128 lanes hold, a step loads A for
@@ -13,7 +14,7 @@ namespace precc {
 
 constexpr int AS_THREADS = 192;                          // producer, MMA issuer, four epilogue warps
 constexpr int AS_LANES = 128;
-constexpr int AS_MAX_STAGES = 8;
+constexpr int AS_MAX_STAGES = 24;
 template <bool Q8>
 constexpr int AS_CHUNKS = Q8 ? 2 : 4;                    // accumulators of a pass at most
 template <bool Q8>
@@ -27,6 +28,8 @@ __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t
       ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// What bounds a block is the latency of its copies against the bytes it has in flight, so a slot of the ring holds the lanes that are used and no more
+// (the MMA reads 128 lanes whatever lies behind them; 16 KB behind the ring are kept for the last slot's).
 // p.BN: rows of a block (a multiple of 16, at most 256 / 128 where more than one accumulator is used); ring_bytes: shared memory for the ring
 template <bool Q8>
 __global__ void __launch_bounds__(AS_THREADS, 1)
@@ -36,50 +39,55 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ __align__(8) uint64_t bars[2 * AS_MAX_STAGES + 2];
   __shared__ uint32_t tmem_holder;
-  __shared__ int8_t row_agent[256];
+  __shared__ __align__(16) int8_t row_agent[256];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int TN = p.BN;
-  const long long m0 = (long long)blockIdx.x * TN;
+  const int TN = p.BN, KS = gridDim.x, rank_c = blockIdx.x;          // the cluster spans grid.x
+  const long long m0 = (long long)blockIdx.y * TN;
+  float* part = reinterpret_cast<float*>(smem + ring_bytes + AS_LANES * AP_ROW_BYTES);         // KS > 1: [TN][rank_pad]
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * AS_MAX_STAGES, acc_full = empty0 + 8 * AS_MAX_STAGES, acc_empty = acc_full + 8;
-  const int nkb = p.K / (Q8 ? 128 : 64);
+  const int nkb_all = p.K / (Q8 ? 128 : 64);
+  const int kb0 = (int)((long long)rank_c * nkb_all / KS), nkb = (int)((long long)(rank_c + 1) * nkb_all / KS) - kb0;
   if (threadIdx.x == 0) {
+    prefetch_map(&map_x);
+    prefetch_map(&map_a);
     for (int s = 0; s < AS_MAX_STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     mbar_init(acc_full, 1);
     mbar_init(acc_empty, 4);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
   }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_holder)), "r"(p.tmem_cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
   pdl_wait();
   pdl_launch_dependents();
   int id[8];
-  const unsigned long long present = agents_of_rows(p, m0, TN, lane, id);
-  if (warp == 2) {
+  load_agents(p, m0, lane, id);
+  bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      row_agent[32 * i + lane] = (int8_t)max(id[i], -1);
-      const long long m = m0 + 32 * i + lane;
-      if (32 * i + lane < TN && m < p.M && (p.agent_id[m] < -1 || p.agent_id[m] >= p.n_agents)) atomicOr(p.status, StatusBits::BAD_INDEX);
-    }
+  for (int i = 0; i < 8; ++i) bad |= 32 * i + lane < TN && m0 + 32 * i + lane < p.M && (id[i] < -1 || id[i] >= p.n_agents);
+  const unsigned long long present = agents_present(p, m0, TN, lane, id);
+  if (warp == 2) {
+    if (bad && rank_c == 0) atomicOr(p.status, StatusBits::BAD_INDEX);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) row_agent[32 * i + lane] = (int8_t)id[i];
   }
-  if (present == 0) return;                              // (the same in every thread)
-  const int slots = AS_LANES / p.rank;                   // agents in an accumulator
-  const int all_chunks = (__popcll(present) + slots - 1) / slots;
-  const int chunks = min(all_chunks, min(AS_CHUNKS<Q8>, 512 / TN));       // accumulators of a pass
-  const int x_bytes = TN * AP_ROW_BYTES, stage_bytes = (x_bytes + 1023) / 1024 * 1024 + chunks * AS_CHUNK_BYTES<Q8>;
-  const int stages = min(AS_MAX_STAGES, ring_bytes / stage_bytes);
+  // (no agents: nothing is loaded, multiplied or written, and the same in every thread of the cluster)
+  const int slots = AS_LANES / p.rank, n_present = __popcll(present);               // slots: agents in an accumulator
+  const int all_chunks = (n_present + slots - 1) / slots;
+  // accumulators of a pass: what tensor memory holds, and what leaves room for two slots of the ring (one always fits once, see launch_shrink_tc)
+  const int room = (ring_bytes / 2 - TN * AP_ROW_BYTES) / AS_CHUNK_BYTES<Q8>;
+  const int chunks = max(1, min(min(all_chunks, room), min(AS_CHUNKS<Q8>, p.tmem_cols / TN)));
   const int passes = (all_chunks + chunks - 1) / chunks;
-  uint32_t tmem_cols = 32;
-  while ((int)tmem_cols < chunks * TN) tmem_cols <<= 1;
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_holder)), "r"(tmem_cols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
-  }
+  const int lane_bytes = (all_chunks > 1 ? AS_LANES : n_present * p.rank) * AP_ROW_BYTES, chunk_bytes = lane_bytes * (Q8 ? 2 : 1);
+  const int a_off = TN * AP_ROW_BYTES, stage_bytes = a_off + chunks * chunk_bytes;  // (TN: a multiple of 16)
+  const int stages = min(AS_MAX_STAGES, ring_bytes / stage_bytes);
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
   const uint32_t tmem_base = tmem_holder;
   const uint32_t smem0 = smem_u32(smem);
-  const int a_off = (x_bytes + 1023) / 1024 * 1024;
   // takes the agents of the next pass off `rest`
   auto next_pass = [&](unsigned long long& rest) {
     unsigned long long now = 0;
@@ -88,58 +96,60 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   };
 
   if (warp == 0) {
-    RingWalk at;
-    unsigned long long rest = present;
-    for (int pass = 0; pass < passes; ++pass) {
-      const unsigned long long now = next_pass(rest);
-      const uint32_t tx = x_bytes + __popcll(now) * p.rank * AP_ROW_BYTES * (Q8 ? 2 : 1);
-      for (int kb = 0; kb < nkb; ++kb, at.next(stages)) {
-        if (at.filled) mbar_wait(empty0 + 8 * at.s, at.parity ^ 1u, p.status);
-        const uint32_t st = smem0 + at.s * stage_bytes, bar = full0 + 8 * at.s;
-        if (elect_one()) {
+    if (elect_one()) {
+      RingWalk at;
+      unsigned long long rest = present;
+      for (int pass = 0; pass < passes; ++pass) {
+        const unsigned long long now = next_pass(rest);
+        const uint32_t tx = (TN + __popcll(now) * p.rank * (Q8 ? 2 : 1)) * AP_ROW_BYTES;
+        for (int kb = 0; kb < nkb; ++kb, at.next(stages)) {
+          if (at.filled) mbar_wait(empty0 + 8 * at.s, at.parity ^ 1u, p.status);
+          const uint32_t st = smem0 + at.s * stage_bytes, bar = full0 + 8 * at.s;
           mbar_expect_tx(bar, tx);
-          tma_load_2d(st, &map_x, kb * (Q8 ? 128 : 64), (int)m0, bar);
-          int i = 0;
-          for (unsigned long long left = now; left; left &= left - 1, ++i) {
+          tma_load_3d(st, &map_x, 0, (int)m0, kb0 + kb, bar);
+          uint32_t dst = st + a_off;
+          int slot = 0;
+          for (unsigned long long left = now; left; left &= left - 1) {
             const int row = (__ffsll(left) - 1) * p.rank;
-            const uint32_t dst = st + a_off + i / slots * AS_CHUNK_BYTES<Q8> + i % slots * p.rank * AP_ROW_BYTES;
-            tma_load_3d(dst, &map_a, 0, row, kb, bar);
-            if constexpr (Q8) tma_load_3d(dst + AS_LANES * AP_ROW_BYTES, &map_a, 0, p.n_agents * p.rank + row, kb, bar);
+            tma_load_3d(dst, &map_a, 0, row, kb0 + kb, bar);
+            if constexpr (Q8) tma_load_3d(dst + lane_bytes, &map_a, 0, p.n_agents * p.rank + row, kb0 + kb, bar);
+            dst += p.rank * AP_ROW_BYTES;
+            if (++slot == slots) { slot = 0; dst += chunk_bytes - lane_bytes; }
           }
         }
-        __syncwarp();
       }
     }
+    __syncwarp();
   } else if (warp == 1) {
     const uint32_t idesc = Q8 ? umma_idesc_bf16(TN) & ~((1u << 7) | (1u << 10)) : umma_idesc_bf16(TN);      // (e4m3 is format 0)
     const uint64_t dx0 = umma_desc_sw128(smem0), da0 = umma_desc_sw128(smem0 + a_off);
-    RingWalk at;
-    for (int pass = 0; pass < passes; ++pass) {
-      if (pass > 0) mbar_wait(acc_empty, (pass - 1) & 1, p.status);
-      const int live = min(chunks, all_chunks - pass * chunks);
-      for (int kb = 0; kb < nkb; ++kb, at.next(stages)) {
-        mbar_wait(full0 + 8 * at.s, at.parity, p.status);
-        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-        if (elect_one()) {
+    if (elect_one()) {
+      RingWalk at;
+      for (int pass = 0; pass < passes; ++pass) {
+        if (pass > 0) mbar_wait(acc_empty, (pass - 1) & 1, p.status);
+        const int live = min(chunks, all_chunks - pass * chunks);
+        for (int kb = 0; kb < nkb; ++kb, at.next(stages)) {
+          mbar_wait(full0 + 8 * at.s, at.parity, p.status);
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
           const uint64_t so = (uint64_t)((at.s * stage_bytes) >> 4);
           for (int c = 0; c < live; ++c) {
-            const uint64_t da = da0 + so + (uint64_t)((c * AS_CHUNK_BYTES<Q8>) >> 4);
+            const uint64_t da = da0 + so + (uint64_t)(c * chunk_bytes >> 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               if constexpr (Q8) {
                 umma_e4m3(tmem_base + c * TN, da + 2 * k, dx0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
-                umma_e4m3(tmem_base + c * TN, da + ((AS_LANES * AP_ROW_BYTES) >> 4) + 2 * k, dx0 + so + 2 * k, idesc, 1u);
+                umma_e4m3(tmem_base + c * TN, da + (lane_bytes >> 4) + 2 * k, dx0 + so + 2 * k, idesc, 1u);
               } else {
                 umma_bf16(tmem_base + c * TN, da + 2 * k, dx0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
               }
             }
           }
           umma_commit(empty0 + 8 * at.s);
-          if (kb == nkb - 1) umma_commit(acc_full);
         }
-        __syncwarp();
+        umma_commit(acc_full);
       }
     }
+    __syncwarp();
   } else {
     const int quad = warp & 3, slot = (quad * 32 + lane) / p.rank, coord = (quad * 32 + lane) % p.rank;
     unsigned long long rest = present;
@@ -154,16 +164,25 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
           if (i == slot) agent = __ffsll(now) - 1;
         float scale = p.s;
         if constexpr (Q8) { if (agent >= 0) scale *= p.a_scale[agent * p.rank + coord]; }
-        for (int r0 = 0; r0 < TN; r0 += 16) {
+        if (!__any_sync(0xffffffffu, agent >= 0)) continue;
+        __nv_bfloat16* t_row = p.T + m0 * p.rank_pad + coord;
+        float* part_row = part + coord;
+        for (int r0 = 0; r0 < TN; r0 += 16, t_row += 16 * p.rank_pad, part_row += 16 * p.rank_pad) {
           uint32_t v[16];
           tmem_ld16(tmem_base + c * TN + r0 + (static_cast<uint32_t>(quad * 32) << 16), v);
+          const uint4 who = *reinterpret_cast<const uint4*>(row_agent + r0);         // sixteen rows' agents
           asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
-            if (row_agent[r0 + q] != agent) continue;
-            __nv_bfloat16* dst = p.T + (m0 + r0 + q) * p.rank_pad + coord;
-            *dst = __float2bfloat16(scale * __uint_as_float(v[q]));
-            if (p.rank < p.rank_pad) dst[p.rank] = __float2bfloat16(0.f);       // (rank 8 of 16)
+            const uint32_t four = q < 4 ? who.x : q < 8 ? who.y : q < 12 ? who.z : who.w;
+            const bool on = (int)(int8_t)(four >> (8 * (q & 3))) == agent;
+            const float x = scale * __uint_as_float(v[q]);
+            if (KS > 1) {
+              if (on) part_row[q * p.rank_pad] = x;
+            } else if (on) {
+              t_row[q * p.rank_pad] = __float2bfloat16(x);
+              if (p.rank < p.rank_pad) t_row[q * p.rank_pad + p.rank] = __float2bfloat16(0.f);       // (rank 8 of 16)
+            }
           }
         }
       }
@@ -174,9 +193,31 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
+  if (KS > 1) {                                          // every block finishes a share of the elements
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    for (int i = rank_c * AS_THREADS + threadIdx.x; i < TN * p.rank_pad; i += KS * AS_THREADS) {
+      const int r = i / p.rank_pad, c = i % p.rank_pad;
+      if (row_agent[r] < 0) continue;
+      float v = 0.f;
+      if (c < p.rank) {
+        const uint32_t local = smem_u32(part + i);
+        for (int k = 0; k < KS; ++k) {
+          float u;
+          asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(u) : "r"(dsmem_addr(local, k)));
+          v += u;
+        }
+      }
+      p.T[(m0 + r) * p.rank_pad + c] = __float2bfloat16(v);
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");      // nobody leaves while its sums are read
+  }
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base), "r"(tmem_cols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base), "r"(p.tmem_cols) : "memory");
   }
 }
 

@@ -64,6 +64,8 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   const bool adapters = p.agent_id != nullptr;
 
   if (threadIdx.x == 0) {
+    prefetch_map(&map_w);
+    prefetch_map(&map_x);
     for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     mbar_init(acc_full, 1);
     mbar_init(ready_bar, KS > 1 ? KS - 1 : 1);
@@ -73,10 +75,10 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     if (!adapters) pdl_wait();                           // with adapters the shrink kernel is ahead and has waited
     for (int it = 0; it < min(p.stages, nkb_s); ++it) {
-      const uint32_t st = smem_u32(smem) + it * stage_bytes;
+      const uint32_t st = smem0 + it * stage_bytes;
       mbar_expect_tx(full0 + 8 * it, stage_bytes);
       tma_load_3d(st, &map_w, 0, n0, kb0 + it, full0 + 8 * it);
-      tma_load_2d(st + PT_W_BYTES, &map_x, (kb0 + it) * STEP, m0, full0 + 8 * it);
+      tma_load_3d(st + PT_W_BYTES, &map_x, 0, m0, kb0 + it, full0 + 8 * it);
     }
   }
   if (warp == 1) {
@@ -93,17 +95,15 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
 
   if (warp == 0) {
-    RingWalk at;                                         // (the first round was requested above)
-    for (int it = p.stages; it < nkb_s; ++it, at.next(p.stages)) {
-      const int s = at.s;
-      mbar_wait(empty0 + 8 * s, at.parity, p.status);
-      const uint32_t st = smem0 + s * stage_bytes;
-      if (elect_one()) {
-        mbar_expect_tx(full0 + 8 * s, stage_bytes);
-        tma_load_3d(st, &map_w, 0, n0, kb0 + it, full0 + 8 * s);
-        tma_load_2d(st + PT_W_BYTES, &map_x, (kb0 + it) * STEP, m0, full0 + 8 * s);
+    if (elect_one()) {
+      RingWalk at;                                       // (the first round was requested above)
+      for (int it = p.stages; it < nkb_s; ++it, at.next(p.stages)) {
+        const uint32_t st = smem0 + at.s * stage_bytes, bar = full0 + 8 * at.s;
+        mbar_wait(empty0 + 8 * at.s, at.parity, p.status);
+        mbar_expect_tx(bar, stage_bytes);
+        tma_load_3d(st, &map_w, 0, n0, kb0 + it, bar);
+        tma_load_3d(st + PT_W_BYTES, &map_x, 0, m0, kb0 + it, bar);
       }
-      __syncwarp();
     }
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
@@ -111,22 +111,20 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     const uint32_t idesc = Q8 ? umma_idesc_bf16(TN) & ~((1u << 7) | (1u << 10)) : umma_idesc_bf16(TN);     // (e4m3 is format 0)
     const uint64_t dw0 = umma_desc_sw128(smem0);
     const uint64_t dx0 = umma_desc_sw128(smem0 + PT_W_BYTES);
-    RingWalk at;
-    for (int it = 0; it < nkb_s; ++it, at.next(p.stages)) {
-      const int s = at.s;
-      mbar_wait(full0 + 8 * s, at.parity, p.status);
-      asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-      if (elect_one()) {
-        const uint64_t so = (uint64_t)((s * stage_bytes) >> 4);
+    if (elect_one()) {
+      RingWalk at;
+      for (int it = 0; it < nkb_s; ++it, at.next(p.stages)) {
+        mbar_wait(full0 + 8 * at.s, at.parity, p.status);
+        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+        const uint64_t so = (uint64_t)((at.s * stage_bytes) >> 4);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {                    // 32 bytes of K a step
           if constexpr (Q8) umma_e4m3(tmem_base, dw0 + so + 2 * k, dx0 + so + 2 * k, idesc, (it | k) ? 1u : 0u);
           else umma_bf16(tmem_base, dw0 + so + 2 * k, dx0 + so + 2 * k, idesc, (it | k) ? 1u : 0u);
         }
-        umma_commit(empty0 + 8 * s);
-        if (it == nkb_s - 1) umma_commit(acc_full);      // every MMA of the slice has completed: the ring is idle too
+        umma_commit(empty0 + 8 * at.s);
       }
-      __syncwarp();
+      umma_commit(acc_full);                             // every MMA of the slice has completed: the ring is idle too
     }
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");

@@ -100,11 +100,12 @@ int32_t encode(precc_ctx* ctx, CUtensorMap* map, CUtensorMapDataType type, int r
   if (r != CUDA_SUCCESS) return fail(ctx, PRECC_ERR_CUDA, "cuTensorMapEncodeTiled (adapted projection) failed (%d)", (int)r);
   return PRECC_OK;
 }
-// Rows of X, and packed weights [K / step][N][step], in steps of 128 bytes of K.
+// Rows of X, and packed weights [K / step][N][step], as k-blocks of 128 bytes: a box is `box_rows` rows of one k-block.
 int32_t map_rows(precc_ctx* ctx, CUtensorMap* map, const void* x, int M, int K, int box_rows, bool q8) {
-  const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)M}, strides[1] = {(cuuint64_t)K * (q8 ? 1 : 2)};
-  const cuuint32_t box[2] = {q8 ? 128u : 64u, (cuuint32_t)box_rows};
-  return encode(ctx, map, q8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, x, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+  const cuuint32_t step = q8 ? 128 : 64;
+  const cuuint64_t dims[3] = {step, (cuuint64_t)M, (cuuint64_t)K / step}, strides[2] = {(cuuint64_t)K * (q8 ? 1 : 2), 128};
+  const cuuint32_t box[3] = {step, (cuuint32_t)box_rows, 1};
+  return encode(ctx, map, q8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, x, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 int32_t map_weights(precc_ctx* ctx, CUtensorMap* map, const void* w, int N, int K, int box_rows, bool q8) {
   const cuuint32_t step = q8 ? 128 : 64;
@@ -147,16 +148,29 @@ int32_t launch_shrink(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
 int env_int(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 0; }
 
 template <bool Q8>
-int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
+int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, int smem_free, cudaStream_t stream) {
+  const int nkb = p.K / (Q8 ? 128 : 64);
   const int rounds = (p.M + ctx->sm_count * 256 - 1) / (ctx->sm_count * 256);
   p.BN = ((p.M + ctx->sm_count * rounds - 1) / (ctx->sm_count * rounds) + 15) / 16 * 16;
-  const int ring = ctx->max_smem_optin - 4096, smem = ring + 1024;
+  int ks = 1;
+  if (env_int("AS_TN")) p.BN = env_int("AS_TN");
+  else if (p.M <= 4096) p.BN = std::max(p.BN, std::min(32, (p.M + 15) / 16 * 16));
+  const int tiles = (p.M + p.BN - 1) / p.BN;
+  while (ks < 8 && tiles * ks * 2 <= ctx->sm_count && nkb >= ks * 4) ks *= 2;
+  const int slots = AS_LANES / p.rank, chunks = std::min(AS_CHUNKS<Q8>, (p.n_agents + slots - 1) / slots);
+  p.tmem_cols = 32;
+  while (p.tmem_cols < std::min(chunks * p.BN, 512)) p.tmem_cols <<= 1;
+  // behind the ring: what the MMA of its last slot reads past it, and the sums of a K slice
+  const int tail = AS_LANES * AP_ROW_BYTES + (ks > 1 ? p.BN * p.rank_pad * 4 : 0), most = ctx->max_smem_optin - 4096 - tail;
+  const int slot = p.BN * AP_ROW_BYTES + AS_CHUNK_BYTES<Q8>;                 // with one whole accumulator: 64 KB at most
+  const int ring = std::min(most, std::max(smem_free, 3 * slot));
+  const int smem = ring + tail + 1024;
   CUtensorMap map_x, map_a;
   int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, p.BN, Q8);
   if (!rc) rc = map_weights(ctx, &map_a, p.A, p.n_agents * p.rank * (Q8 ? 2 : 1), p.K, p.rank, Q8);
   if (rc) return rc;
   PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_shrink_tc_kernel<Q8>, smem));
-  Launch l(dim3((unsigned)((p.M + p.BN - 1) / p.BN)), AS_THREADS, smem, 1, stream);
+  Launch l(dim3((unsigned)ks, (unsigned)tiles), AS_THREADS, smem, ks, stream);
   PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_shrink_tc_kernel<Q8>, map_x, map_a, p, ring));
   return PRECC_OK;
 }
@@ -164,7 +178,7 @@ int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
 template <bool Q8>
 int32_t run_shrink(precc_ctx* ctx, const AdaptedParams& p, cudaStream_t stream) {
   const int tc = env_int("AS_TC");
-  if (tc ? p.M >= tc : p.M >= 2048) return launch_shrink_tc<Q8>(ctx, p, stream);
+  if (tc ? p.M >= tc : p.M >= 2048) return launch_shrink_tc<Q8>(ctx, p, env_int("AS_SMEM") ? env_int("AS_SMEM") : 1 << 20, stream);
   const bool few = p.M <= 64;
   switch (p.rank_pad) {
     case 16: return few ? launch_shrink<1, 1, Q8>(ctx, p, stream) : launch_shrink<1, 4, Q8>(ctx, p, stream);
@@ -178,7 +192,6 @@ constexpr int SHRINK_SMEM = 38 * 1024;           // what a block of the shrink k
 template <bool Q8>
 int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t stream) {
   const int m_tiles = (p.M + AP_BM - 1) / AP_BM, pairs_max = ctx->sm_count / 2;
-  const int nkb = p.K / (Q8 ? 128 : 64);
   double best = 1e30;
   for (int bn : {256, 192, 128, 64}) {
     const long long tiles = (long long)m_tiles * ((p.N + bn - 1) / bn);
@@ -200,7 +213,6 @@ int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t st
     map_t = map_b = map_x;
   }
   if (rc) return rc;
-  (void)nkb;
   const long long tiles = (long long)m_tiles * ((p.N + p.BN - 1) / p.BN);
   PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_pair_kernel<Q8>, smem));
   Launch l(dim3((unsigned)(2 * std::min<long long>(tiles, pairs_max))), AP_THREADS, smem, 2, stream);
@@ -239,7 +251,7 @@ int32_t run_turn(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t st
     if (tn == last) { if (tn == 16) break; else continue; }
     last = tn;
     const long long tiles = (p.M + tn - 1) / tn;
-    for (int ks = 1; ks <= GEMM_MAX_KS && nkb >= ks; ++ks) {
+    for (int ks = 1; ks <= GEMM_MAX_KS && ks <= nkb; ++ks) {          // (every block of a cluster has a step)
       if (f_ks && ks != f_ks) continue;
       const int resident = ks == 1 ? ctx->sm_count : fit[ks];
       if (resident < 1) continue;
