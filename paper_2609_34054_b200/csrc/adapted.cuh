@@ -18,6 +18,7 @@ constexpr int AP_ROW_BYTES = 128;             // bytes of K in a step: 64 bf16 o
 
 struct AdaptedParams {
   int M, N, K, rank, rank_pad;                // rank_pad: rank, at least 16 (the K of one MMA)
+  int rank_shift;                             // log2 of rank
   int n_agents;
   const int32_t* agent_id;                    // [M], or null: no adapters in this call
   const void* x;                              // [M][K] bf16 or e4m3
@@ -205,13 +206,15 @@ adapted_shrink_kernel(const AdaptedParams p) {
   for (int i = threadIdx.x + (int)rank_c * SHRINK_THREADS; i < RT * R; i += SHRINK_THREADS * (int)KS) {
     const int r = i / R, c = i % R;
     if (!((with_adapter >> r) & 1u)) continue;
-    float v = 0.f;
     const uint32_t local = smem_u32(&part[r][c]);
-    for (uint32_t k = 0; k < KS; ++k) {
-      float u;
-      asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(u) : "r"(dsmem_addr(local, k)));
-      v += u;
+    float u[8], v = 0.f;
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {             // (asked for at once: one read after the other costs its latency every time)
+      u[k] = 0.f;
+      if (k < KS) asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(u[k]) : "r"(dsmem_addr(local, k)));
     }
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) v += u[k];
     if constexpr (Q8) { if (c < p.rank) v *= p.a_scale[agent_of(p, row0 + r) * p.rank + c]; }
     p.T[(row0 + r) * p.rank_pad + c] = __float2bfloat16(p.s * v);
   }

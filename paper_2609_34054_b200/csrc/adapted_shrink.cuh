@@ -15,6 +15,8 @@ namespace precc {
 constexpr int AS_THREADS = 192;                          // producer, MMA issuer, four epilogue warps
 constexpr int AS_LANES = 128;
 constexpr int AS_MAX_STAGES = 24;
+constexpr int AS_DUMP_ROWS = 64, AS_DUMP_PITCH = AS_LANES + 4;            // (in floats; the pitch spreads a row's pieces over the banks)
+constexpr int AS_TAIL_BYTES = AS_DUMP_ROWS * AS_DUMP_PITCH * 4;
 template <bool Q8>
 constexpr int AS_CHUNKS = Q8 ? 2 : 4;                    // accumulators of a pass at most
 template <bool Q8>
@@ -28,8 +30,10 @@ __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t
       ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// What bounds a block is the latency of its copies against the bytes it has in flight, so a slot of the ring holds the lanes that are used and no more
-// (the MMA reads 128 lanes whatever lies behind them; 16 KB behind the ring are kept for the last slot's).
+// A slot of the ring holds the lanes that are used and no more (the MMA reads 128 lanes whatever lies behind them; the tail behind the ring is larger
+// than what it reads past the last slot).
+// A lane of the accumulator is a coordinate and a column a row, so 64 rows at a time go through shared memory, where each row finds the
+// coordinates of its agent side by side (writing them out of the accumulator, two bytes a row under a condition each, took 3.6 us for 64 rows).
 // p.BN: rows of a block (a multiple of 16, at most 256 / 128 where more than one accumulator is used); ring_bytes: shared memory for the ring
 template <bool Q8>
 __global__ void __launch_bounds__(AS_THREADS, 1)
@@ -43,16 +47,19 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int TN = p.BN, KS = gridDim.x, rank_c = blockIdx.x;          // the cluster spans grid.x
   const long long m0 = (long long)blockIdx.y * TN;
-  float* part = reinterpret_cast<float*>(smem + ring_bytes + AS_LANES * AP_ROW_BYTES);         // KS > 1: [TN][rank_pad]
+  float* dump = reinterpret_cast<float*>(smem + ring_bytes);         // [64 rows][lanes]
+  float* part = reinterpret_cast<float*>(smem + ring_bytes + AS_TAIL_BYTES);         // KS > 1: [TN][rank]
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * AS_MAX_STAGES, acc_full = empty0 + 8 * AS_MAX_STAGES, acc_empty = acc_full + 8;
   const int nkb_all = p.K / (Q8 ? 128 : 64);
   const int kb0 = (int)((long long)rank_c * nkb_all / KS), nkb = (int)((long long)(rank_c + 1) * nkb_all / KS) - kb0;
   if (threadIdx.x == 0) {
     prefetch_map(&map_x);
     prefetch_map(&map_a);
-    for (int s = 0; s < AS_MAX_STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     mbar_init(acc_full, 1);
     mbar_init(acc_empty, 4);
+  }
+  if (warp == 0) {
+    if (lane < AS_MAX_STAGES) { mbar_init(full0 + 8 * lane, 1); mbar_init(empty0 + 8 * lane, 1); }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
   }
@@ -74,8 +81,8 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
     for (int i = 0; i < 8; ++i) row_agent[32 * i + lane] = (int8_t)id[i];
   }
   // (no agents: nothing is loaded, multiplied or written, and the same in every thread of the cluster)
-  const int slots = AS_LANES / p.rank, n_present = __popcll(present);               // slots: agents in an accumulator
-  const int all_chunks = (n_present + slots - 1) / slots;
+  const int slots = AS_LANES >> p.rank_shift, n_present = __popcll(present);        // slots: agents in an accumulator
+  const int all_chunks = (n_present + slots - 1) >> (7 - p.rank_shift);
   // accumulators of a pass: what tensor memory holds, and what leaves room for two slots of the ring (one always fits once, see launch_shrink_tc)
   const int room = (ring_bytes / 2 - TN * AP_ROW_BYTES) / AS_CHUNK_BYTES<Q8>;
   const int chunks = max(1, min(min(all_chunks, room), min(AS_CHUNKS<Q8>, p.tmem_cols / TN)));
@@ -151,7 +158,8 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
     }
     __syncwarp();
   } else {
-    const int quad = warp & 3, slot = (quad * 32 + lane) / p.rank, coord = (quad * 32 + lane) % p.rank;
+    const int quad = warp & 3, et = threadIdx.x - 64;
+    const int pieces = p.rank >> 2;                      // of four coordinates in a row
     unsigned long long rest = present;
     for (int pass = 0; pass < passes; ++pass) {
       unsigned long long now = next_pass(rest);
@@ -159,31 +167,40 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
       mbar_wait_relaxed(acc_full, pass & 1, p.status);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       for (int c = 0; c < live; ++c) {
-        int agent = -2;                                  // of this lane (no row has agent -2)
-        for (int i = 0; i < slots && now; ++i, now &= now - 1)
-          if (i == slot) agent = __ffsll(now) - 1;
-        float scale = p.s;
-        if constexpr (Q8) { if (agent >= 0) scale *= p.a_scale[agent * p.rank + coord]; }
-        if (!__any_sync(0xffffffffu, agent >= 0)) continue;
-        __nv_bfloat16* t_row = p.T + m0 * p.rank_pad + coord;
-        float* part_row = part + coord;
-        for (int r0 = 0; r0 < TN; r0 += 16, t_row += 16 * p.rank_pad, part_row += 16 * p.rank_pad) {
-          uint32_t v[16];
-          tmem_ld16(tmem_base + c * TN + r0 + (static_cast<uint32_t>(quad * 32) << 16), v);
-          const uint4 who = *reinterpret_cast<const uint4*>(row_agent + r0);         // sixteen rows' agents
-          asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+        unsigned long long mine = 0;                     // the agents of this accumulator
+        for (int i = 0; i < slots && now; ++i) { mine |= now & (0 - now); now &= now - 1; }
+        const bool lanes_used = quad * 32 < __popcll(mine) << p.rank_shift;
+        for (int b0 = 0; b0 < TN; b0 += AS_DUMP_ROWS) {
+          const int nb = min(AS_DUMP_ROWS, TN - b0);
+          float* col = dump + quad * 32 + lane;
+          for (int r0 = 0; lanes_used && r0 < nb; r0 += 16, col += 16 * AS_DUMP_PITCH) {
+            uint32_t v[16];
+            tmem_ld16(tmem_base + c * TN + b0 + r0 + (static_cast<uint32_t>(quad * 32) << 16), v);
+            asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
 #pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            const uint32_t four = q < 4 ? who.x : q < 8 ? who.y : q < 12 ? who.z : who.w;
-            const bool on = (int)(int8_t)(four >> (8 * (q & 3))) == agent;
-            const float x = scale * __uint_as_float(v[q]);
+            for (int q = 0; q < 16; ++q) col[q * AS_DUMP_PITCH] = __uint_as_float(v[q]);
+          }
+          asm volatile("bar.sync 1, 128;\n" ::: "memory");
+          for (int i = et; i < nb * pieces; i += 128) {
+            const int r = i >> (p.rank_shift - 2), k = (i & (pieces - 1)) * 4, a = row_agent[b0 + r];
+            if (a < 0 || !((mine >> a) & 1ull)) continue;
+            const int at = __popcll(mine & ((1ull << a) - 1)) << p.rank_shift;
+            float4 v = *reinterpret_cast<const float4*>(dump + r * AS_DUMP_PITCH + at + k);
+            float4 w = make_float4(p.s, p.s, p.s, p.s);
+            if constexpr (Q8) {
+              const float4 sc = *reinterpret_cast<const float4*>(p.a_scale + (a << p.rank_shift) + k);
+              w = make_float4(p.s * sc.x, p.s * sc.y, p.s * sc.z, p.s * sc.w);
+            }
+            v = make_float4(v.x * w.x, v.y * w.y, v.z * w.z, v.w * w.w);
             if (KS > 1) {
-              if (on) part_row[q * p.rank_pad] = x;
-            } else if (on) {
-              t_row[q * p.rank_pad] = __float2bfloat16(x);
-              if (p.rank < p.rank_pad) t_row[q * p.rank_pad + p.rank] = __float2bfloat16(0.f);       // (rank 8 of 16)
+              *reinterpret_cast<float4*>(part + ((b0 + r) << p.rank_shift) + k) = v;
+            } else {
+              __nv_bfloat16* dst = p.T + (m0 + b0 + r) * p.rank_pad + k;
+              *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+              if (p.rank < p.rank_pad) *reinterpret_cast<uint2*>(dst + p.rank) = make_uint2(0u, 0u);       // (rank 8 of 16)
             }
           }
+          asm volatile("bar.sync 1, 128;\n" ::: "memory");
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
@@ -197,19 +214,22 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-    for (int i = rank_c * AS_THREADS + threadIdx.x; i < TN * p.rank_pad; i += KS * AS_THREADS) {
-      const int r = i / p.rank_pad, c = i % p.rank_pad;
+    const int pieces = p.rank >> 2;
+    for (int i = rank_c * AS_THREADS + threadIdx.x; i < TN * pieces; i += KS * AS_THREADS) {
+      const int r = i >> (p.rank_shift - 2), k = (i & (pieces - 1)) * 4;
       if (row_agent[r] < 0) continue;
-      float v = 0.f;
-      if (c < p.rank) {
-        const uint32_t local = smem_u32(part + i);
-        for (int k = 0; k < KS; ++k) {
-          float u;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(u) : "r"(dsmem_addr(local, k)));
-          v += u;
-        }
+      const uint32_t local = smem_u32(part + (r << p.rank_shift) + k);
+      float4 u[8], v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        u[j] = v;
+        if (j < KS) asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(u[j].x), "=f"(u[j].y), "=f"(u[j].z), "=f"(u[j].w) : "r"(dsmem_addr(local, j)));
       }
-      p.T[(m0 + r) * p.rank_pad + c] = __float2bfloat16(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { v.x += u[j].x; v.y += u[j].y; v.z += u[j].z; v.w += u[j].w; }
+      __nv_bfloat16* dst = p.T + (m0 + r) * p.rank_pad + k;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+      if (p.rank < p.rank_pad) *reinterpret_cast<uint2*>(dst + p.rank) = make_uint2(0u, 0u);
     }
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");

@@ -160,9 +160,9 @@ int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, int smem_free, cudaStr
   const int slots = AS_LANES / p.rank, chunks = std::min(AS_CHUNKS<Q8>, (p.n_agents + slots - 1) / slots);
   p.tmem_cols = 32;
   while (p.tmem_cols < std::min(chunks * p.BN, 512)) p.tmem_cols <<= 1;
-  // behind the ring: what the MMA of its last slot reads past it, and the sums of a K slice
-  const int tail = AS_LANES * AP_ROW_BYTES + (ks > 1 ? p.BN * p.rank_pad * 4 : 0), most = ctx->max_smem_optin - 4096 - tail;
-  const int slot = p.BN * AP_ROW_BYTES + AS_CHUNK_BYTES<Q8>;                 // with one whole accumulator: 64 KB at most
+  // behind the ring: 64 rows of an accumulator, and the sums of a K slice
+  const int tail = AS_TAIL_BYTES + (ks > 1 ? p.BN * p.rank * 4 : 0), most = ctx->max_smem_optin - 4096 - tail;
+  const int slot = p.BN * AP_ROW_BYTES + AS_CHUNK_BYTES<Q8>;                 // with one whole accumulator: 64 KB at most, beside a tail of up to 97 KB
   const int ring = std::min(most, std::max(smem_free, 3 * slot));
   const int smem = ring + tail + 1024;
   CUtensorMap map_x, map_a;
@@ -307,7 +307,7 @@ int32_t project(precc_ctx* ctx, const precc_projection* d, const void* X, const 
       (reinterpret_cast<uintptr_t>(a_scale) & 3u) || (reinterpret_cast<uintptr_t>(agent_id) & 3u))
     return fail(ctx, PRECC_ERR_MISALIGNED, "X / W / Y / A / B / w_scale not 16-byte aligned (x_scale, a_scale, agent_id: 4)");
   AdaptedParams p = {};
-  p.M = M; p.N = d->n_out; p.K = d->k_dim; p.rank = d->rank; p.rank_pad = std::max(16, d->rank); p.n_agents = d->n_agents;
+  p.M = M; p.N = d->n_out; p.K = d->k_dim; p.rank = d->rank; p.rank_pad = std::max(16, d->rank); p.rank_shift = d->rank ? __builtin_ctz(d->rank) : 0; p.n_agents = d->n_agents;
   p.x = X; p.x_scale = x_scale; p.w_scale = w_scale; p.y = (__nv_bfloat16*)Y; p.s = d->lora_scale; p.status = ctx->status;
   if (adapters) {
     const size_t need = precc_adapted_ws_bytes(d, M);
