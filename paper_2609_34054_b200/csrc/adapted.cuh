@@ -32,6 +32,7 @@ struct AdaptedParams {
   float s;
   int tile_rows;                              // shrink kernel: rows of a block
   int BN, stages, tmem_cols;
+  int kps;                                    // shrink kernel of many rows: k-blocks in a slot of its ring
   uint32_t* status;
 };
 

@@ -10,7 +10,7 @@
 
 namespace precc {
 
-constexpr int AP_EPI_WARPS = 4;
+constexpr int AP_EPI_WARPS = 8;                       // two on each quarter of the lanes, half of the columns each
 constexpr int AP_THREADS = (2 + AP_EPI_WARPS) * 32;   // producer, MMA issuer, epilogue warps
 constexpr int AP_BM = 2 * GEMM_BM;
 constexpr int AP_A_BYTES = GEMM_BM * AP_ROW_BYTES;
@@ -52,6 +52,7 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   const uint32_t acc_full = empty0 + 8 * p.stages;
   const uint32_t acc_empty = acc_full + 16;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bars + 2 * p.stages + 4);
+  __shared__ __align__(16) float w_scale_s[2][256];       // 8 bits: the scales of a tile's columns
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
@@ -67,7 +68,7 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     if (adapters) { prefetch_map(&map_t); prefetch_map(&map_b); }
     for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     mbar_init(acc_full, 1); mbar_init(acc_full + 8, 1);
-    mbar_init(acc_empty, 8); mbar_init(acc_empty + 8, 8);
+    mbar_init(acc_empty, 2 * AP_EPI_WARPS); mbar_init(acc_empty + 8, 2 * AP_EPI_WARPS);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
   }
@@ -179,7 +180,9 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       }
     }
   } else {
-    const int lane_base = (warp & 3) * 32;
+    // ---- epilogue: a thread holds a row of the accumulator and stores 64 bytes of Y at a time; the next 32 columns are on their way meanwhile
+    const int lane_base = (warp & 3) * 32, et = threadIdx.x - 64;
+    const int c_begin = (warp - 2) / 4 * half_n, c_end = c_begin + half_n;      // (half_n: a multiple of 32)
     const uint32_t acc_empty_lead = map_to_rank(acc_empty, 0);
     int i = 0;
     for (long long t = pair; t < n_tiles; t += n_pairs, ++i) {
@@ -187,28 +190,40 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       const int m = (int)(t / n_tiles_n) * AP_BM + (int)rank * GEMM_BM + lane_base + lane, n0 = (int)(t % n_tiles_n) * p.BN;
       const bool row_ok = m < p.M;
       float xs = 1.f;
-      if constexpr (Q8) xs = row_ok ? p.x_scale[m] : 0.f;
+      if constexpr (Q8) {
+        if (et < p.BN) w_scale_s[buf][et] = n0 + et < p.N ? p.w_scale[n0 + et] : 0.f;
+        xs = row_ok ? p.x_scale[m] : 0.f;
+        asm volatile("bar.sync 1, 256;\n" ::: "memory");       // (a buffer is written again two tiles later, behind another of these)
+      }
       __nv_bfloat16* yr = p.y + (long long)m * p.N + n0;
       mbar_wait_relaxed(acc_full + 8 * buf, (i >> 1) & 1, p.status);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       const uint32_t acc = tmem_base + buf * p.BN + (static_cast<uint32_t>(lane_base) << 16);
-      for (int c0 = 0; c0 < p.BN && n0 + c0 < p.N; c0 += 16) {
-        uint32_t r[16];
-        tmem_ld16(acc + c0, r);
-        asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+      auto store = [&](const uint32_t (&r)[32], int c) {
+        if (!row_ok) return;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!row_ok || n0 + c0 + 8 * h >= p.N) continue;       // (N is a multiple of 8)
+        for (int q = 0; q < 4; ++q) {
           float v[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[8 * h + k]);
+          for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[8 * q + k]);
           if constexpr (Q8) {
-            const float4* ws = reinterpret_cast<const float4*>(p.w_scale + n0 + c0 + 8 * h);
-            const float4 u = __ldg(ws), w = __ldg(ws + 1);
+            const float4 u = *reinterpret_cast<const float4*>(&w_scale_s[buf][c + 8 * q]), w = *reinterpret_cast<const float4*>(&w_scale_s[buf][c + 8 * q + 4]);
             v[0] *= xs * u.x; v[1] *= xs * u.y; v[2] *= xs * u.z; v[3] *= xs * u.w;
             v[4] *= xs * w.x; v[5] *= xs * w.y; v[6] *= xs * w.z; v[7] *= xs * w.w;
           }
-          *reinterpret_cast<uint4*>(yr + c0 + 8 * h) = pack_bf16x8(v);
+          if (n0 + c + 8 * q < p.N) *reinterpret_cast<uint4*>(yr + c + 8 * q) = pack_bf16x8(v);       // (N is a multiple of 8)
+        }
+      };
+      uint32_t r0[32], r1[32];
+      tmem_ld32(acc + c_begin, r0);
+      for (int c = c_begin; c < c_end; c += 64) {
+        asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+        if (c + 32 < c_end) tmem_ld32(acc + c + 32, r1);
+        store(r0, c);
+        if (c + 32 < c_end) {
+          asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+          if (c + 64 < c_end) tmem_ld32(acc + c + 64, r0);
+          store(r1, c + 32);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");

@@ -30,7 +30,8 @@ __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t
       ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// A slot of the ring holds the lanes that are used and no more (the MMA reads 128 lanes whatever lies behind them; the tail behind the ring is larger
+// A slot of the ring holds `kps` neighbouring k-blocks, which one copy fetches as up to 512 bytes of every row (128 bytes a row and copy leave DRAM at
+// two thirds of its rate), and of A the lanes that are used and no more (the MMA reads 128 lanes whatever lies behind them; the tail behind the ring is larger
 // than what it reads past the last slot).
 // A lane of the accumulator is a coordinate and a column a row, so 64 rows at a time go through shared memory, where each row finds the
 // coordinates of its agent side by side (writing them out of the accumulator, two bytes a row under a condition each, took 3.6 us for 64 rows).
@@ -50,8 +51,8 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   float* dump = reinterpret_cast<float*>(smem + ring_bytes);         // [64 rows][lanes]
   float* part = reinterpret_cast<float*>(smem + ring_bytes + AS_TAIL_BYTES);         // KS > 1: [TN][rank]
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * AS_MAX_STAGES, acc_full = empty0 + 8 * AS_MAX_STAGES, acc_empty = acc_full + 8;
-  const int nkb_all = p.K / (Q8 ? 128 : 64);
-  const int kb0 = (int)((long long)rank_c * nkb_all / KS), nkb = (int)((long long)(rank_c + 1) * nkb_all / KS) - kb0;
+  const int steps_all = (p.K / (Q8 ? 128 : 64) + p.kps - 1) / p.kps;               // (k-blocks past K arrive as zeros)
+  const int step0 = (int)((long long)rank_c * steps_all / KS), steps = (int)((long long)(rank_c + 1) * steps_all / KS) - step0;
   if (threadIdx.x == 0) {
     prefetch_map(&map_x);
     prefetch_map(&map_a);
@@ -84,11 +85,12 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   const int slots = AS_LANES >> p.rank_shift, n_present = __popcll(present);        // slots: agents in an accumulator
   const int all_chunks = (n_present + slots - 1) >> (7 - p.rank_shift);
   // accumulators of a pass: what tensor memory holds, and what leaves room for two slots of the ring (one always fits once, see launch_shrink_tc)
-  const int room = (ring_bytes / 2 - TN * AP_ROW_BYTES) / AS_CHUNK_BYTES<Q8>;
+  const int room = (ring_bytes / (2 * p.kps) - TN * AP_ROW_BYTES) / AS_CHUNK_BYTES<Q8>;
   const int chunks = max(1, min(min(all_chunks, room), min(AS_CHUNKS<Q8>, p.tmem_cols / TN)));
   const int passes = (all_chunks + chunks - 1) / chunks;
   const int lane_bytes = (all_chunks > 1 ? AS_LANES : n_present * p.rank) * AP_ROW_BYTES, chunk_bytes = lane_bytes * (Q8 ? 2 : 1);
-  const int a_off = TN * AP_ROW_BYTES, stage_bytes = a_off + chunks * chunk_bytes;  // (TN: a multiple of 16)
+  const int a_off = p.kps * TN * AP_ROW_BYTES, a_bytes = chunks * chunk_bytes;      // (TN: a multiple of 16)
+  const int stage_bytes = a_off + p.kps * a_bytes;
   const int stages = min(AS_MAX_STAGES, ring_bytes / stage_bytes);
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
@@ -108,20 +110,23 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
       unsigned long long rest = present;
       for (int pass = 0; pass < passes; ++pass) {
         const unsigned long long now = next_pass(rest);
-        const uint32_t tx = (TN + __popcll(now) * p.rank * (Q8 ? 2 : 1)) * AP_ROW_BYTES;
-        for (int kb = 0; kb < nkb; ++kb, at.next(stages)) {
+        const uint32_t tx = p.kps * (TN + __popcll(now) * p.rank * (Q8 ? 2 : 1)) * AP_ROW_BYTES;
+        for (int it = 0; it < steps; ++it, at.next(stages)) {
           if (at.filled) mbar_wait(empty0 + 8 * at.s, at.parity ^ 1u, p.status);
           const uint32_t st = smem0 + at.s * stage_bytes, bar = full0 + 8 * at.s;
+          const int kb = (step0 + it) * p.kps;
           mbar_expect_tx(bar, tx);
-          tma_load_3d(st, &map_x, 0, (int)m0, kb0 + kb, bar);
-          uint32_t dst = st + a_off;
-          int slot = 0;
-          for (unsigned long long left = now; left; left &= left - 1) {
-            const int row = (__ffsll(left) - 1) * p.rank;
-            tma_load_3d(dst, &map_a, 0, row, kb0 + kb, bar);
-            if constexpr (Q8) tma_load_3d(dst + lane_bytes, &map_a, 0, p.n_agents * p.rank + row, kb0 + kb, bar);
-            dst += p.rank * AP_ROW_BYTES;
-            if (++slot == slots) { slot = 0; dst += chunk_bytes - lane_bytes; }
+          tma_load_3d(st, &map_x, 0, (int)m0, kb, bar);
+          for (int j = 0; j < p.kps; ++j) {
+            uint32_t dst = st + a_off + j * a_bytes;
+            int slot = 0;
+            for (unsigned long long left = now; left; left &= left - 1) {
+              const int row = (__ffsll(left) - 1) << p.rank_shift;
+              tma_load_3d(dst, &map_a, 0, row, kb + j, bar);
+              if constexpr (Q8) tma_load_3d(dst + lane_bytes, &map_a, 0, p.n_agents * p.rank + row, kb + j, bar);
+              dst += p.rank * AP_ROW_BYTES;
+              if (++slot == slots) { slot = 0; dst += chunk_bytes - lane_bytes; }
+            }
           }
         }
       }
@@ -135,19 +140,21 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
       for (int pass = 0; pass < passes; ++pass) {
         if (pass > 0) mbar_wait(acc_empty, (pass - 1) & 1, p.status);
         const int live = min(chunks, all_chunks - pass * chunks);
-        for (int kb = 0; kb < nkb; ++kb, at.next(stages)) {
+        for (int it = 0; it < steps; ++it, at.next(stages)) {
           mbar_wait(full0 + 8 * at.s, at.parity, p.status);
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-          const uint64_t so = (uint64_t)((at.s * stage_bytes) >> 4);
-          for (int c = 0; c < live; ++c) {
-            const uint64_t da = da0 + so + (uint64_t)(c * chunk_bytes >> 4);
+          uint64_t dx = dx0 + (uint64_t)((at.s * stage_bytes) >> 4), da_step = da0 + (uint64_t)((at.s * stage_bytes) >> 4);
+          for (int j = 0; j < p.kps; ++j, dx += TN * AP_ROW_BYTES >> 4, da_step += a_bytes >> 4) {
+            uint64_t da = da_step;
+            for (int c = 0; c < live; ++c, da += chunk_bytes >> 4) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if constexpr (Q8) {
-                umma_e4m3(tmem_base + c * TN, da + 2 * k, dx0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
-                umma_e4m3(tmem_base + c * TN, da + (lane_bytes >> 4) + 2 * k, dx0 + so + 2 * k, idesc, 1u);
-              } else {
-                umma_bf16(tmem_base + c * TN, da + 2 * k, dx0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
+              for (int k = 0; k < 4; ++k) {
+                if constexpr (Q8) {
+                  umma_e4m3(tmem_base + c * TN, da + 2 * k, dx + 2 * k, idesc, (it | j | k) ? 1u : 0u);
+                  umma_e4m3(tmem_base + c * TN, da + (lane_bytes >> 4) + 2 * k, dx + 2 * k, idesc, 1u);
+                } else {
+                  umma_bf16(tmem_base + c * TN, da + 2 * k, dx + 2 * k, idesc, (it | j | k) ? 1u : 0u);
+                }
               }
             }
           }

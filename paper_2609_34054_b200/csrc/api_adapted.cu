@@ -100,11 +100,12 @@ int32_t encode(precc_ctx* ctx, CUtensorMap* map, CUtensorMapDataType type, int r
   if (r != CUDA_SUCCESS) return fail(ctx, PRECC_ERR_CUDA, "cuTensorMapEncodeTiled (adapted projection) failed (%d)", (int)r);
   return PRECC_OK;
 }
-// Rows of X, and packed weights [K / step][N][step], as k-blocks of 128 bytes: a box is `box_rows` rows of one k-block.
-int32_t map_rows(precc_ctx* ctx, CUtensorMap* map, const void* x, int M, int K, int box_rows, bool q8) {
+// Rows of X, and packed weights [K / step][N][step], as k-blocks of 128 bytes: a box is `box_rows` rows of one k-block (of
+// X, also of several, one behind the other; those past K arrive as zeros).
+int32_t map_rows(precc_ctx* ctx, CUtensorMap* map, const void* x, int M, int K, int box_rows, bool q8, int blocks = 1) {
   const cuuint32_t step = q8 ? 128 : 64;
   const cuuint64_t dims[3] = {step, (cuuint64_t)M, (cuuint64_t)K / step}, strides[2] = {(cuuint64_t)K * (q8 ? 1 : 2), 128};
-  const cuuint32_t box[3] = {step, (cuuint32_t)box_rows, 1};
+  const cuuint32_t box[3] = {step, (cuuint32_t)box_rows, (cuuint32_t)blocks};
   return encode(ctx, map, q8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, x, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 int32_t map_weights(precc_ctx* ctx, CUtensorMap* map, const void* w, int N, int K, int box_rows, bool q8) {
@@ -162,11 +163,16 @@ int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, int smem_free, cudaStr
   while (p.tmem_cols < std::min(chunks * p.BN, 512)) p.tmem_cols <<= 1;
   // behind the ring: 64 rows of an accumulator, and the sums of a K slice
   const int tail = AS_TAIL_BYTES + (ks > 1 ? p.BN * p.rank * 4 : 0), most = ctx->max_smem_optin - 4096 - tail;
-  const int slot = p.BN * AP_ROW_BYTES + AS_CHUNK_BYTES<Q8>;                 // with one whole accumulator: 64 KB at most, beside a tail of up to 97 KB
+  p.kps = 4;                                     // k-blocks in a slot: as many as leave three slots and every block two of them to do
+  if (env_int("AS_KPS")) p.kps = env_int("AS_KPS");
+  const int typical = p.BN * AP_ROW_BYTES + std::min(p.n_agents, 2) * p.rank * AP_ROW_BYTES * (Q8 ? 2 : 1);
+  const int whole = p.BN * AP_ROW_BYTES + AS_CHUNK_BYTES<Q8>;                // with all lanes of one accumulator: 64 KB at most, beside a tail of up to 97 KB
+  while (p.kps > 1 && (3 * p.kps * typical > most || p.kps * whole > most || nkb < 2 * ks * p.kps)) p.kps /= 2;
+  const int slot = p.kps * whole;
   const int ring = std::min(most, std::max(smem_free, 3 * slot));
   const int smem = ring + tail + 1024;
   CUtensorMap map_x, map_a;
-  int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, p.BN, Q8);
+  int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, p.BN, Q8, p.kps);
   if (!rc) rc = map_weights(ctx, &map_a, p.A, p.n_agents * p.rank * (Q8 ? 2 : 1), p.K, p.rank, Q8);
   if (rc) return rc;
   PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_shrink_tc_kernel<Q8>, smem));
@@ -199,7 +205,7 @@ int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t st
     if (cost < best - 1e-9) { best = cost; p.BN = bn; }
   }
   const int stage = ap_stage_bytes(p.BN);
-  p.stages = std::min(8, (ctx->max_smem_optin - 2048 - (p.agent_id ? SHRINK_SMEM : 0)) / stage);
+  p.stages = std::min(8, (ctx->max_smem_optin - 4096 - (p.agent_id ? SHRINK_SMEM : 0)) / stage);
   p.tmem_cols = 32;
   while (p.tmem_cols < 2 * p.BN) p.tmem_cols <<= 1;
   const int smem = p.stages * stage + (2 * p.stages + 6) * 8 + 1024;
