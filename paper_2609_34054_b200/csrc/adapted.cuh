@@ -110,12 +110,14 @@ template <int MT, int NT, bool Q8>
 __global__ void __launch_bounds__(SHRINK_THREADS, 2)
 adapted_shrink_kernel(const AdaptedParams p) {
   constexpr int RT = 8 * NT, R = 16 * MT;
-  __shared__ float red[SHRINK_WARPS][RT][R];
+  constexpr int MW = MT > 2 ? 2 : MT, KW = SHRINK_WARPS * MW / MT;      // pieces of the rank of a warp; warps that share the K extent
+  __shared__ float red[KW][RT][R];
   __shared__ float part[RT][R];
   uint32_t rank_c, KS;
   asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank_c));
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;\n" : "=r"(KS));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int kw = warp % KW, m0 = warp / KW * MW;
   const long long row0 = (long long)(blockIdx.x / KS) * p.tile_rows;
   pdl_wait();
   pdl_launch_dependents();
@@ -134,48 +136,46 @@ adapted_shrink_kernel(const AdaptedParams p) {
   const int a_rows = p.n_agents * p.rank;
   const long long row_bytes = (long long)p.K * (Q8 ? 1 : 2);
 
-  while (todo) {
-    const int a = __shfl_sync(0xffffffffu, id, __ffs(todo) - 1);
-    const unsigned mine = __ballot_sync(0xffffffffu, id == a);
-    todo &= ~mine;
-    float acc[MT][NT][4];
+  // step v of agent a: fragments of this warp's part of A, and of the rows of that agent
+  auto fetch = [&](int a, unsigned mine, int v, uint4 (&av)[MW][2][2], uint4 (&xv)[NT][2]) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MW; ++m)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) { acc[m][n][0] = acc[m][n][1] = acc[m][n][2] = acc[m][n][3] = 0.f; }
-#pragma unroll 2
-    for (int v = v0 + warp; v < v1; v += SHRINK_WARPS) {
-      uint4 av[MT][2][2];
+      for (int h = 0; h < 2; ++h) {
+        const int r = (m0 + m) * 16 + h * 8 + g;
+        const uint4* src = static_cast<const uint4*>(p.A) + ((long long)v * a_rows + a * p.rank + r) * 8;      // (step v = value or rest of k-block v / 2)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = m * 16 + h * 8 + g;
-          const uint4* src = static_cast<const uint4*>(p.A) + ((long long)v * a_rows + a * p.rank + r) * 8;      // (step v = value or rest of k-block v / 2)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) av[m][h][c] = r < p.rank ? __ldg(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
-        }
-      uint4 xv[NT][2];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const bool on = (mine >> (n * 8 + g)) & 1u;
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (row0 + n * 8 + g) * row_bytes + (long long)(v / PARTS) * AP_ROW_BYTES);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) xv[n][c] = on ? __ldg(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
+        for (int c = 0; c < 2; ++c) av[m][h][c] = r < p.rank ? __ldg(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+    for (int n = 0; n < NT; ++n) {
+      const bool on = (mine >> (n * 8 + g)) & 1u;
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (row0 + n * 8 + g) * row_bytes + (long long)(v / PARTS) * AP_ROW_BYTES);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            const uint32_t a0[4] = {av[m][0][c].x, av[m][1][c].x, av[m][0][c].y, av[m][1][c].y};
-            const uint32_t a1[4] = {av[m][0][c].z, av[m][1][c].z, av[m][0][c].w, av[m][1][c].w};
-            mma_step<Q8>(acc[m][n], a0, xv[n][c].x, xv[n][c].y);
-            mma_step<Q8>(acc[m][n], a1, xv[n][c].z, xv[n][c].w);
-          }
+      for (int c = 0; c < 2; ++c) xv[n][c] = on ? __ldg(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
     }
-    // a row belongs to one agent: its column goes to its place once
+  };
+  float acc[MW][NT][4];
+  auto clear = [&]() {
+#pragma unroll
+    for (int m = 0; m < MW; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) { acc[m][n][0] = acc[m][n][1] = acc[m][n][2] = acc[m][n][3] = 0.f; }
+  };
+  auto multiply = [&](const uint4 (&av)[MW][2][2], const uint4 (&xv)[NT][2]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MW; ++m) {
+          const uint32_t a0[4] = {av[m][0][c].x, av[m][1][c].x, av[m][0][c].y, av[m][1][c].y};
+          const uint32_t a1[4] = {av[m][0][c].z, av[m][1][c].z, av[m][0][c].w, av[m][1][c].w};
+          mma_step<Q8>(acc[m][n], a0, xv[n][c].x, xv[n][c].y);
+          mma_step<Q8>(acc[m][n], a1, xv[n][c].z, xv[n][c].w);
+        }
+  };
+  auto leave = [&](unsigned mine) {                // a row belongs to one agent: its column goes to its place once
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -183,9 +183,50 @@ adapted_shrink_kernel(const AdaptedParams p) {
         const int r = n * 8 + 2 * t + e;
         if ((mine >> r) & 1u) {
 #pragma unroll
-          for (int m = 0; m < MT; ++m) { red[warp][r][m * 16 + g] = acc[m][n][e]; red[warp][r][m * 16 + 8 + g] = acc[m][n][2 + e]; }
+          for (int m = 0; m < MW; ++m) { red[kw][r][(m0 + m) * 16 + g] = acc[m][n][e]; red[kw][r][(m0 + m) * 16 + 8 + g] = acc[m][n][2 + e]; }
         }
       }
+  };
+  auto next_agent = [&](unsigned& mine) {          // -1: none left
+    mine = 0;
+    if (!todo) return -1;
+    const int a = __shfl_sync(0xffffffffu, id, __ffs(todo) - 1);
+    mine = __ballot_sync(0xffffffffu, id == a);
+    todo &= ~mine;
+    return a;
+  };
+  unsigned mine;
+  int a = next_agent(mine);
+  clear();
+  if constexpr (NT == 1) {
+    // few rows, so often an agent of its own for each: the next step's fragments, be it of the next agent, are on their way while one is multiplied
+    uint4 a0[MW][2][2], x0[NT][2], a1[MW][2][2], x1[NT][2];
+    int v = v0 + kw;
+    if (v >= v1) { while (a >= 0) { leave(mine); a = next_agent(mine); } }
+    if (a >= 0) fetch(a, mine, v, a0, x0);
+    auto step = [&](const uint4 (&av)[MW][2][2], const uint4 (&xv)[NT][2], uint4 (&an)[MW][2][2], uint4 (&xn)[NT][2]) {
+      const unsigned now = mine;
+      const bool last = v + KW >= v1;
+      if (last) { a = next_agent(mine); v = v0 + kw; } else { v += KW; }
+      if (a >= 0) fetch(a, mine, v, an, xn);
+      multiply(av, xv);
+      if (last) { leave(now); clear(); }
+    };
+    while (a >= 0) {
+      step(a0, x0, a1, x1);
+      if (a >= 0) step(a1, x1, a0, x0);
+    }
+  } else {
+    for (; a >= 0; a = next_agent(mine)) {
+#pragma unroll 2
+      for (int v = v0 + kw; v < v1; v += KW) {
+        uint4 av[MW][2][2], xv[NT][2];
+        fetch(a, mine, v, av, xv);
+        multiply(av, xv);
+      }
+      leave(mine);
+      clear();
+    }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < RT * R; i += SHRINK_THREADS) {
@@ -193,7 +234,7 @@ adapted_shrink_kernel(const AdaptedParams p) {
     float v = 0.f;
     if ((with_adapter >> r) & 1u) {
 #pragma unroll
-      for (int w = 0; w < SHRINK_WARPS; ++w) v += red[w][r][c];
+      for (int w = 0; w < KW; ++w) v += red[w][r][c];
     }
     part[r][c] = v;
   }

@@ -23,6 +23,9 @@ __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   return v;
 }
 
+template <int NT, int MT>
+constexpr int AF_U = MT == 1 && NT == 2 ? 2 : 3;
+
 __host__ __device__ constexpr int af_smem_bytes(int nt, int mt, int rank_pad) {
   return (AF_WARPS + 1) * 8 * nt * (16 * mt + 4) * 4 + AF_WARPS * rank_pad * (32 * mt + 16);
 }
@@ -33,7 +36,7 @@ __global__ void __launch_bounds__(AF_THREADS, MT == 1 ? 2 : 1)
 adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
   constexpr int C = 16 * MT, S = C + 4;           // row of the partial sums, padded: the lanes of a store hit 32 banks
   constexpr int BP = C * 2 + 16;                  // bytes of a row of a B slice, padded for ldmatrix
-  constexpr int U = MT == 1 && NT == 2 ? 2 : 3;   // k-blocks of a warp in flight
+  constexpr int U = AF_U<NT, MT>;                 // k-blocks of a warp in flight
   extern __shared__ __align__(16) uint8_t smem[];
   float (*red)[8 * NT][S] = reinterpret_cast<float (*)[8 * NT][S]>(smem);                    // [warp]
   float (*low)[S] = red[AF_WARPS];                                                           // s (x A) B of every row

@@ -36,7 +36,7 @@ __device__ __forceinline__ void umma_pair_bf16_lanes(uint32_t tmem_d, uint64_t d
 }
 
 template <bool Q8>
-__global__ void __launch_bounds__(AP_THREADS, 1)
+__global__ void __launch_bounds__(AP_THREADS, 2)
 adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                     const __grid_constant__ CUtensorMap map_t, const __grid_constant__ CUtensorMap map_b, const AdaptedParams p) {
   extern __shared__ unsigned char smem_raw[];

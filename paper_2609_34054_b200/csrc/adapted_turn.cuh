@@ -6,7 +6,8 @@
 // main loop runs), and a warp multiplies a group's rows of T with 64 columns of that agent's B by mma.sync: rows of different agents never share a
 // product.  B comes straight from global memory: a lane reads eight neighbouring columns of the four coordinates that the fragment wants
 // of it, and column 8 g + j belongs to column g of the j-th MMA, so that it holds sixteen neighbouring columns of the result.
-// The product of a warp's first group is taken before the sums are there.
+// Where a block has few rows the products are taken while the main loop runs, into a place of their own; else a warp's first one is, in registers, and
+// all are added to the sums in shared memory.
 #pragma once
 #include "adapted_shrink.cuh"
 
@@ -25,12 +26,14 @@ struct AtTables {
   int n_groups;
 };
 
+constexpr int AT_LOW_ROWS = 32;                          // own rows of a block whose adapters' share has a place beside the ring
+__host__ __device__ constexpr int at_low_bytes(int tn, int ks) { return pt_share(tn, ks) <= AT_LOW_ROWS ? AT_LOW_ROWS * PT_COLS * 4 : 0; }
 __host__ __device__ constexpr int at_smem_bytes(int tn, int ks, int stages) {
-  return pt_data_bytes(tn, ks, stages, 1) + ((int)sizeof(AtTables) + 15) / 16 * 16 + (2 * PT_MAX_STAGES + 4) * 8;
+  return pt_data_bytes(tn, ks, stages, 1) + at_low_bytes(tn, ks) + ((int)sizeof(AtTables) + 15) / 16 * 16 + (2 * PT_MAX_STAGES + 4) * 8;
 }
 
 template <bool Q8>
-__global__ void __launch_bounds__(AT_THREADS, 1)
+__global__ void __launch_bounds__(AT_THREADS, 2)
 adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const AdaptedParams p) {
   extern __shared__ __align__(1024) unsigned char smem[];
   if ((smem_u32(smem) & 1023u) != 0) {                   // the swizzle atoms and the peers' addresses rely on it
@@ -42,8 +45,10 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   const int TN = p.BN;
   const int stage_bytes = pt_stage_bytes(TN, 1);
   constexpr int STEP = Q8 ? 128 : 64;
-  AtTables& tab = *reinterpret_cast<AtTables*>(smem + pt_data_bytes(TN, KS, p.stages, 1));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + pt_data_bytes(TN, KS, p.stages, 1) + (sizeof(AtTables) + 15) / 16 * 16);
+  const int low_bytes = at_low_bytes(TN, KS);
+  float* low = reinterpret_cast<float*>(smem + pt_data_bytes(TN, KS, p.stages, 1));           // [own rows][128], where they are few
+  AtTables& tab = *reinterpret_cast<AtTables*>(reinterpret_cast<unsigned char*>(low) + low_bytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<unsigned char*>(&tab) + (sizeof(AtTables) + 15) / 16 * 16);
   const uint32_t full0 = smem_u32(bars);
   const uint32_t empty0 = full0 + 8 * PT_MAX_STAGES;
   const uint32_t acc_full = empty0 + 8 * PT_MAX_STAGES;
@@ -142,34 +147,44 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       const __nv_bfloat16* t1 = p.T + (long long)(m0 + rank * tw + r1) * p.rank_pad + 2 * t;
 #pragma unroll
       for (int j = 0; j < 8; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
-      for (int k0 = 0; k0 < p.rank_pad; k0 += 16) {
-        uint4 b[4];
+      const __nv_bfloat16* src = p.B + ((long long)a * p.rank + 2 * t) * p.N + n;
+      auto fetch = [&](int k0, uint4 (&b)[4], uint32_t (&f)[4]) {        // coordinates k0 .. k0 + 15
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int r = k0 + 2 * t + (k & 1) + 8 * (k >> 1);
+          const int r = k0 + (k & 1) + 8 * (k >> 1);
           b[k] = make_uint4(0, 0, 0, 0);
-          if (r < p.rank && n < p.N) b[k] = __ldg(reinterpret_cast<const uint4*>(p.B + ((long long)a * p.rank + r) * p.N + n));
+          if (2 * t + r < p.rank && n < p.N) b[k] = __ldg(reinterpret_cast<const uint4*>(src + (long long)r * p.N));
         }
-        uint32_t f[4];
         f[0] = r0 != AT_NO_ROW ? *reinterpret_cast<const uint32_t*>(t0 + k0) : 0u;
         f[1] = r1 != AT_NO_ROW ? *reinterpret_cast<const uint32_t*>(t1 + k0) : 0u;
         f[2] = r0 != AT_NO_ROW ? *reinterpret_cast<const uint32_t*>(t0 + k0 + 8) : 0u;
         f[3] = r1 != AT_NO_ROW ? *reinterpret_cast<const uint32_t*>(t1 + k0 + 8) : 0u;
+      };
+      auto multiply = [&](const uint4 (&b)[4], const uint32_t (&f)[4]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           auto word = [&](int k) { return j < 2 ? b[k].x : j < 4 ? b[k].y : j < 6 ? b[k].z : b[k].w; };
           const uint32_t pick = j & 1 ? 0x7632 : 0x5410;
           mma_bf16_16816(d[j], f, __byte_perm(word(0), word(1), pick), __byte_perm(word(2), word(3), pick));
         }
+      };
+      uint4 b0[4], b1[4];                                // the next sixteen coordinates are on their way while sixteen are multiplied
+      uint32_t f0[4], f1[4];
+      fetch(0, b0, f0);
+      for (int k0 = 0; k0 < p.rank_pad; k0 += 32) {
+        if (k0 + 16 < p.rank_pad) fetch(k0 + 16, b1, f1);
+        multiply(b0, f0);
+        if (k0 + 32 < p.rank_pad) fetch(k0 + 32, b0, f0);
+        if (k0 + 16 < p.rank_pad) multiply(b1, f1);
       }
     };
-    auto add_product = [&](int u) {
+    auto add_product = [&](int u, float* to) {           // to: the block's own rows
       const int gr = u >> 1;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int r = tab.rows[gr][g + 8 * e];
         if (r == AT_NO_ROW) continue;
-        float* row = dump + (size_t)(rank * tw + r) * PT_COLS + (u & 1) * 64 + 16 * t;
+        float* row = to + (size_t)r * PT_COLS + (u & 1) * 64 + 16 * t;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {                    // columns 4 q .. of the lane's sixteen
           float4 v = *reinterpret_cast<float4*>(row + 4 * q);
@@ -218,7 +233,14 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       pdl_wait();                                        // T is complete (in every block, so that this grid ends after the shrink kernel)
       if (et == 0) pdl_launch_dependents();
     }
-    if (ew < n_units) product(ew);
+    const bool early = low_bytes > 0 && n_units > 0;
+    if (early) {
+      for (int i = et; i < own_rows * PT_COLS / 4; i += 256) reinterpret_cast<float4*>(low)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      sync_merging();
+      for (int u = ew; u < n_units; u += AT_EPI_WARPS) { product(u); add_product(u, low); }
+    } else if (ew < n_units) {
+      product(ew);
+    }
 
     asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");       // the peers' barriers are initialised
     mbar_wait(acc_full, 0, p.status);
@@ -260,9 +282,10 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       }
     }
     // ---- the adapters' share of the own rows
-    if (ew < n_units) {
-      add_product(ew);
-      for (int u = ew + AT_EPI_WARPS; u < n_units; u += AT_EPI_WARPS) { product(u); add_product(u); }
+    if (!early && ew < n_units) {
+      float* own = dump + (size_t)rank * tw * PT_COLS;
+      add_product(ew, own);
+      for (int u = ew + AT_EPI_WARPS; u < n_units; u += AT_EPI_WARPS) { product(u); add_product(u, own); }
     }
     if (n_units > 0) sync_merging();
     // ---- own rows + received rows, in rank order: sixteen threads per row, eight columns each
@@ -280,6 +303,10 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = 0.f;
+        if (early) {
+          const float4 a = *reinterpret_cast<const float4*>(low + r * PT_COLS + piece * 8), b = *reinterpret_cast<const float4*>(low + r * PT_COLS + piece * 8 + 4);
+          v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        }
 #pragma unroll
         for (int s = 0; s < GEMM_MAX_KS; ++s) {
           if (s < KS) {
