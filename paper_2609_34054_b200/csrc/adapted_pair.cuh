@@ -12,6 +12,7 @@ namespace precc {
 
 constexpr int AP_EPI_WARPS = 8;                       // two on each quarter of the lanes, half of the columns each
 constexpr int AP_THREADS = (2 + AP_EPI_WARPS) * 32;   // producer, MMA issuer, epilogue warps
+constexpr int AP_MAX_STAGES = 8;
 constexpr int AP_BM = 2 * GEMM_BM;
 constexpr int AP_A_BYTES = GEMM_BM * AP_ROW_BYTES;
 
@@ -52,6 +53,8 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   const uint32_t acc_full = empty0 + 8 * p.stages;
   const uint32_t acc_empty = acc_full + 16;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bars + 2 * p.stages + 4);
+  __shared__ int slot_agents[AP_MAX_STAGES];              // of the tile that begins in this slot
+  __shared__ __align__(16) uint32_t slot_lanes[AP_MAX_STAGES][8];   // of an adapter's step: the lanes that are not its agent's
   __shared__ __align__(16) float w_scale_s[2][256];       // 8 bits: the scales of a tile's columns
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -85,19 +88,23 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   if (!adapters) pdl_launch_dependents();
 
   if (warp == 0) {
+    // ---- producer.  It also tells the issuer, slot by slot, how many agents a tile has and which lanes are theirs, so that the issuing thread never waits for
+    // anything but its barriers (worked out there, between two tiles, it cost 5 % of a tile in 8 bits).
     const uint32_t full0_lead = map_to_rank(full0, 0);
     RingWalk at;
     bool waited = false;
+    int id[8];
+    if (adapters && pair < n_tiles) load_agents(p, (long long)(pair / n_tiles_n) * AP_BM, lane, id);
     for (long long t = pair; t < n_tiles; t += n_pairs) {
       const int mt = (int)(t / n_tiles_n) * AP_BM;
       const int m0 = mt + (int)rank * GEMM_BM, n0 = (int)(t % n_tiles_n) * p.BN + (int)rank * half_n;
-      int id[8];
-      if (adapters) load_agents(p, mt, lane, id);
+      const unsigned long long present = adapters ? agents_present(p, mt, AP_BM, lane, id) : 0ull;
       if (elect_one()) {
         RingWalk w = at;
         for (int kb = 0; kb < nkb; ++kb, w.next(p.stages)) {
           if (w.filled) mbar_wait(empty0 + 8 * w.s, w.parity ^ 1u, p.status);
           const uint32_t sa = smem0 + w.s * stage_bytes, bar = full0_lead + 8 * w.s;
+          if (kb == 0) slot_agents[w.s] = __popcll(present);
           if (rank == 0) mbar_expect_tx(full0 + 8 * w.s, step_tx);
           tma_pair_load_3d(sa, &map_x, 0, m0, kb, bar);
           tma_pair_load_3d(sa + AP_A_BYTES, &map_w, 0, n0, kb, bar);
@@ -111,74 +118,66 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         pdl_launch_dependents();
         waited = true;
       }
-      const unsigned long long present = agents_present(p, mt, AP_BM, lane, id);
-      if (elect_one()) {
-        RingWalk w = at;
-        for (unsigned long long left = present; left; left &= left - 1, w.next(p.stages)) {
-          if (w.filled) mbar_wait(empty0 + 8 * w.s, w.parity ^ 1u, p.status);
-          const uint32_t sa = smem0 + w.s * stage_bytes, bar = full0_lead + 8 * w.s;
-          if (rank == 0) mbar_expect_tx(full0 + 8 * w.s, 2u * (GEMM_BM + b_boxes * 64) * p.rank_pad * 2);
-          tma_pair_load_2d(sa, &map_t, 0, m0, bar);
-          for (int j = 0; j < b_boxes; ++j)
-            tma_pair_load_3d(sa + AP_A_BYTES + j * p.rank_pad * 128, &map_b, n0 + 64 * j, 0, __ffsll(left) - 1, bar);
+      for (unsigned long long left = present; left; left &= left - 1, at.next(p.stages)) {
+        const int a = __ffsll(left) - 1;
+        if (at.filled) mbar_wait(empty0 + 8 * at.s, at.parity ^ 1u, p.status);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t off = ~__ballot_sync(0xffffffffu, id[j] == a);
+          if (lane == j) slot_lanes[at.s][j] = off;
         }
+        __syncwarp();
+        if (elect_one()) {
+          const uint32_t sa = smem0 + at.s * stage_bytes, bar = full0_lead + 8 * at.s;
+          if (rank == 0) mbar_expect_tx(full0 + 8 * at.s, 2u * (GEMM_BM + b_boxes * 64) * p.rank_pad * 2);
+          tma_pair_load_2d(sa, &map_t, 0, m0, bar);
+          for (int j = 0; j < b_boxes; ++j) tma_pair_load_3d(sa + AP_A_BYTES + j * p.rank_pad * 128, &map_b, n0 + 64 * j, 0, a, bar);
+        }
+        __syncwarp();
       }
-      __syncwarp();
-      at.skip(__popcll(present), p.stages);
+      if (t + n_pairs < n_tiles) load_agents(p, (t + n_pairs) / n_tiles_n * AP_BM, lane, id);
     }
   } else if (warp == 1) {
-    if (rank == 0) {
+    if (rank == 0 && elect_one()) {
       const uint32_t idesc = Q8 ? umma_pair_idesc_bf16(p.BN) & ~((1u << 7) | (1u << 10)) : umma_pair_idesc_bf16(p.BN);   // (e4m3 is format 0)
       const uint32_t idesc_b = umma_pair_idesc_bf16(p.BN) | (1u << 16);                                                 // B operand MN-major
       const uint64_t da0 = umma_desc_sw128(smem0);
       const uint64_t db0 = umma_desc_sw128(smem0 + AP_A_BYTES);
       const uint64_t dt0 = umma_desc_kmajor(smem0, p.rank_pad * 2);
       const uint64_t de0 = umma_desc_mnmajor(smem0 + AP_A_BYTES, 128, p.rank_pad * 128);
-      RingWalk at;
+      RingWalk w;
       int i = 0;
       for (long long t = pair; t < n_tiles; t += n_pairs, ++i) {
         const int buf = i & 1;
-        const int mt = (int)(t / n_tiles_n) * AP_BM;
-        int id[8];
-        if (adapters) load_agents(p, mt, lane, id);
         const uint32_t d = tmem_base + buf * p.BN;
-        if (elect_one()) {
-          if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
-          RingWalk w = at;
-          for (int kb = 0; kb < nkb; ++kb, w.next(p.stages)) {
-            mbar_wait(full0 + 8 * w.s, w.parity, p.status);
-            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-            const uint64_t so = (uint64_t)((w.s * stage_bytes) >> 4);
+        if (i >= 2) mbar_wait(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, p.status);
+        int agents = 0;
+        for (int kb = 0; kb < nkb; ++kb, w.next(p.stages)) {
+          mbar_wait(full0 + 8 * w.s, w.parity, p.status);
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          const uint64_t so = (uint64_t)((w.s * stage_bytes) >> 4);
+          if (kb == 0) agents = slot_agents[w.s];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {             // 32 bytes of K a step: 16 bf16 or 32 e4m3
-              if constexpr (Q8) umma_pair_e4m3(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
-              else umma_pair_bf16(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
-            }
-            umma_pair_commit_both(empty0 + 8 * w.s);
+          for (int k = 0; k < 4; ++k) {             // 32 bytes of K a step: 16 bf16 or 32 e4m3
+            if constexpr (Q8) umma_pair_e4m3(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
+            else umma_pair_bf16(d, da0 + so + 2 * k, db0 + so + 2 * k, idesc, (kb | k) ? 1u : 0u);
           }
+          umma_pair_commit_both(empty0 + 8 * w.s);
         }
-        __syncwarp();
-        at.skip(nkb, p.stages);
-        const unsigned long long present = adapters ? agents_present(p, mt, AP_BM, lane, id) : 0ull;
-        for (unsigned long long left = present; left; left &= left - 1, at.next(p.stages)) {
-          const int a = __ffsll(left) - 1;
+        for (; agents > 0; --agents, w.next(p.stages)) {
+          mbar_wait(full0 + 8 * w.s, w.parity, p.status);
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          const uint64_t so = (uint64_t)((w.s * stage_bytes) >> 4);
           uint32_t off[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) off[j] = ~__ballot_sync(0xffffffffu, id[j] == a);
-          if (elect_one()) {
-            mbar_wait(full0 + 8 * at.s, at.parity, p.status);
-            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-            const uint64_t so = (uint64_t)((at.s * stage_bytes) >> 4);
-            for (int k = 0; k < p.rank_pad / 16; ++k)
-              umma_pair_bf16_lanes(d, dt0 + so + 2 * k, de0 + so + 128 * k, idesc_b, off);
-            umma_pair_commit_both(empty0 + 8 * at.s);
-          }
-          __syncwarp();
+          for (int j = 0; j < 8; ++j) off[j] = slot_lanes[w.s][j];
+          for (int k = 0; k < p.rank_pad / 16; ++k) umma_pair_bf16_lanes(d, dt0 + so + 2 * k, de0 + so + 128 * k, idesc_b, off);
+          umma_pair_commit_both(empty0 + 8 * w.s);
         }
-        if (elect_one()) umma_pair_commit_both(acc_full + 8 * buf);
-        __syncwarp();
+        umma_pair_commit_both(acc_full + 8 * buf);
       }
     }
+    __syncwarp();
   } else {
     // ---- epilogue: a thread holds a row of the accumulator and stores 64 bytes of Y at a time; the next 32 columns are on their way meanwhile
     const int lane_base = (warp & 3) * 32, et = threadIdx.x - 64;

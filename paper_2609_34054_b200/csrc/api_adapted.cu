@@ -182,9 +182,8 @@ int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, int smem_free, cudaStr
 }
 
 template <bool Q8>
-int32_t run_shrink(precc_ctx* ctx, const AdaptedParams& p, cudaStream_t stream) {
-  const int tc = env_int("AS_TC");
-  if (tc ? p.M >= tc : p.M >= 2048) return launch_shrink_tc<Q8>(ctx, p, env_int("AS_SMEM") ? env_int("AS_SMEM") : 1 << 20, stream);
+int32_t run_shrink(precc_ctx* ctx, const AdaptedParams& p, bool tc, cudaStream_t stream) {
+  if (tc) return launch_shrink_tc<Q8>(ctx, p, env_int("AS_SMEM") ? env_int("AS_SMEM") : 1 << 20, stream);
   const bool few = p.M <= 64;
   switch (p.rank_pad) {
     case 16: return few ? launch_shrink<1, 1, Q8>(ctx, p, stream) : launch_shrink<1, 4, Q8>(ctx, p, stream);
@@ -196,7 +195,7 @@ int32_t run_shrink(precc_ctx* ctx, const AdaptedParams& p, cudaStream_t stream) 
 constexpr int SHRINK_SMEM = 38 * 1024;           // what a block of the shrink kernel takes at most: left free beside the main kernel
 
 template <bool Q8>
-int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t stream) {
+int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, bool beside_shrink, cudaStream_t stream) {
   const int m_tiles = (p.M + AP_BM - 1) / AP_BM, pairs_max = ctx->sm_count / 2;
   double best = 1e30;
   for (int bn : {256, 192, 128, 64}) {
@@ -205,7 +204,7 @@ int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t st
     if (cost < best - 1e-9) { best = cost; p.BN = bn; }
   }
   const int stage = ap_stage_bytes(p.BN);
-  p.stages = std::min(8, (ctx->max_smem_optin - 4096 - (p.agent_id ? SHRINK_SMEM : 0)) / stage);
+  p.stages = std::min(AP_MAX_STAGES, (ctx->max_smem_optin - 4096 - (beside_shrink ? SHRINK_SMEM : 0)) / stage);
   p.tmem_cols = 32;
   while (p.tmem_cols < 2 * p.BN) p.tmem_cols <<= 1;
   const int smem = p.stages * stage + (2 * p.stages + 6) * 8 + 1024;
@@ -243,10 +242,10 @@ int32_t run_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaStrea
 }
 
 template <bool Q8>
-int32_t run_turn(precc_ctx* ctx, AdaptedParams p, const void* W, cudaStream_t stream) {
+int32_t run_turn(precc_ctx* ctx, AdaptedParams p, const void* W, bool beside_shrink, cudaStream_t stream) {
   const int nkb = p.K / (Q8 ? 128 : 64);
   const int* fit = turn_clusters(ctx);
-  const int limit = ctx->max_smem_optin - (p.agent_id ? SHRINK_SMEM : 0);
+  const int limit = ctx->max_smem_optin - (beside_shrink ? SHRINK_SMEM : 0);
   const int groups = (p.N + PT_COLS - 1) / PT_COLS;
   const int f_tn = env_int("AT_TN"), f_ks = env_int("AT_KS");
   int best_tn = 0, best_ks = 0, best_st = 0;
@@ -324,14 +323,16 @@ int32_t project(precc_ctx* ctx, const precc_projection* d, const void* X, const 
   rc = check_device(ctx);
   if (rc) return rc;
   cudaStream_t st = (cudaStream_t)stream;
+  const bool tc = adapters && (env_int("AS_TC") ? M >= env_int("AS_TC") : M >= 2048);
   if (adapters) {
-    rc = run_shrink<Q8>(ctx, p, st);
+    rc = run_shrink<Q8>(ctx, p, tc, st);
     if (rc) return rc;
   }
+  const bool beside = adapters && !tc;
   const int kind = env_int("AP_KIND"), turn_max = env_int("AP_TURN_MAX") ? env_int("AP_TURN_MAX") : 1024;
   if ((M <= AF_MAX_ROWS && kind == 0) || kind == 1) return run_few<Q8>(ctx, p, W, st);
-  if ((M <= turn_max && kind == 0) || kind == 2) return run_turn<Q8>(ctx, p, W, st);
-  return run_pair<Q8>(ctx, p, W, st);
+  if ((M <= turn_max && kind == 0) || kind == 2) return run_turn<Q8>(ctx, p, W, beside, st);
+  return run_pair<Q8>(ctx, p, W, beside, st);
 }
 
 }  // namespace
