@@ -8,13 +8,11 @@
 // T is rounded to bf16, the operand type of the MMA that takes it: 2^-8 of the adapter's term, which is added to a sum that is
 // rounded to bf16 as a whole.
 #pragma once
+#include "adapted_plan.h"
 #include "norm.cuh"
 #include "tc_common.cuh"
 
 namespace precc {
-
-constexpr int AP_MAX_AGENTS = 64;
-constexpr int AP_ROW_BYTES = 128;             // bytes of K in a step: 64 bf16 or 128 e4m3
 
 struct AdaptedParams {
   int M, N, K, rank, rank_pad;                // rank_pad: rank, at least 16 (the K of one MMA)

@@ -14,7 +14,6 @@ namespace precc {
 
 constexpr int AF_WARPS = 8;
 constexpr int AF_THREADS = AF_WARPS * 32;
-constexpr int AF_MAX_ROWS = 16;
 
 // Weights are read once: past L1.
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {

@@ -12,13 +12,6 @@ namespace precc {
 
 constexpr int AP_EPI_WARPS = 8;                       // two on each quarter of the lanes, half of the columns each
 constexpr int AP_THREADS = (2 + AP_EPI_WARPS) * 32;   // producer, MMA issuer, epilogue warps
-constexpr int AP_MAX_STAGES = 8;
-constexpr int AP_BM = 2 * GEMM_BM;
-constexpr int AP_A_BYTES = GEMM_BM * AP_ROW_BYTES;
-
-__host__ __device__ constexpr int ap_w_bytes(int bn) { return (bn / 2 + 63) / 64 * 64 * AP_ROW_BYTES; }   // (a step of B takes whole boxes of 64 columns)
-__host__ __device__ constexpr int ap_stage_bytes(int bn) { return AP_A_BYTES + ap_w_bytes(bn); }
-
 __device__ __forceinline__ void umma_pair_e4m3(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"

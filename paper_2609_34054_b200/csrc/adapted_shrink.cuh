@@ -13,14 +13,6 @@
 namespace precc {
 
 constexpr int AS_THREADS = 192;                          // producer, MMA issuer, four epilogue warps
-constexpr int AS_LANES = 128;
-constexpr int AS_MAX_STAGES = 24;
-constexpr int AS_DUMP_ROWS = 64, AS_DUMP_PITCH = AS_LANES + 4;            // (in floats; the pitch spreads a row's pieces over the banks)
-constexpr int AS_TAIL_BYTES = AS_DUMP_ROWS * AS_DUMP_PITCH * 4;
-template <bool Q8>
-constexpr int AS_CHUNKS = Q8 ? 2 : 4;                    // accumulators of a pass at most
-template <bool Q8>
-constexpr int AS_CHUNK_BYTES = AS_LANES * AP_ROW_BYTES * (Q8 ? 2 : 1);
 
 __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -46,8 +38,10 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   __shared__ uint32_t tmem_holder;
   __shared__ __align__(16) int8_t row_agent[256];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int TN = p.BN, KS = gridDim.x, rank_c = blockIdx.x;          // the cluster spans grid.x
-  const long long m0 = (long long)blockIdx.y * TN;
+  uint32_t KS_u;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;\n" : "=r"(KS_u));
+  const int TN = p.BN, KS = (int)KS_u, rank_c = (int)cluster_ctarank();
+  const long long m0 = (long long)(blockIdx.x / KS) * TN;
   float* dump = reinterpret_cast<float*>(smem + ring_bytes);         // [64 rows][lanes]
   float* part = reinterpret_cast<float*>(smem + ring_bytes + AS_TAIL_BYTES);         // KS > 1: [TN][rank]
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * AS_MAX_STAGES, acc_full = empty0 + 8 * AS_MAX_STAGES, acc_empty = acc_full + 8;
@@ -84,9 +78,9 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
   // (no agents: nothing is loaded, multiplied or written, and the same in every thread of the cluster)
   const int slots = AS_LANES >> p.rank_shift, n_present = __popcll(present);        // slots: agents in an accumulator
   const int all_chunks = (n_present + slots - 1) >> (7 - p.rank_shift);
-  // accumulators of a pass: what tensor memory holds, and what leaves room for two slots of the ring (one always fits once, see launch_shrink_tc)
-  const int room = (ring_bytes / (2 * p.kps) - TN * AP_ROW_BYTES) / AS_CHUNK_BYTES<Q8>;
-  const int chunks = max(1, min(min(all_chunks, room), min(AS_CHUNKS<Q8>, p.tmem_cols / TN)));
+  // accumulators of a pass: what tensor memory holds, and what leaves room for two slots of the ring (one always fits once, see plan_shrink_tc)
+  const int room = (ring_bytes / (2 * p.kps) - TN * AP_ROW_BYTES) / as_chunk_bytes(Q8);
+  const int chunks = max(1, min(min(all_chunks, room), min(as_chunks(Q8), p.tmem_cols / TN)));
   const int passes = (all_chunks + chunks - 1) / chunks;
   const int lane_bytes = (all_chunks > 1 ? AS_LANES : n_present * p.rank) * AP_ROW_BYTES, chunk_bytes = lane_bytes * (Q8 ? 2 : 1);
   const int a_off = p.kps * TN * AP_ROW_BYTES, a_bytes = chunks * chunk_bytes;      // (TN: a multiple of 16)

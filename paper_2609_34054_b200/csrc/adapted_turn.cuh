@@ -13,24 +13,7 @@
 
 namespace precc {
 
-constexpr int AT_EPI_WARPS = 8;
 constexpr int AT_THREADS = (2 + AT_EPI_WARPS) * 32;      // producer, MMA issuer, eight merging warps
-constexpr int AT_NO_ROW = 0xffff;
-constexpr int AT_MAX_GROUPS = PT_MAX_TN / 16 + AP_MAX_AGENTS;
-
-struct AtTables {
-  uint16_t rows[AT_MAX_GROUPS][16];                      // rows of a group (AT_NO_ROW: none), counted among the block's own rows
-  uint8_t agent[AT_MAX_GROUPS];
-  uint8_t of_warp[AT_EPI_WARPS][AP_MAX_AGENTS];          // rows of an agent among the 32 of a warp
-  uint8_t first[AP_MAX_AGENTS];                          // first group of an agent
-  int n_groups;
-};
-
-constexpr int AT_LOW_ROWS = 32;                          // own rows of a block whose adapters' share has a place beside the ring
-__host__ __device__ constexpr int at_low_bytes(int tn, int ks) { return pt_share(tn, ks) <= AT_LOW_ROWS ? AT_LOW_ROWS * PT_COLS * 4 : 0; }
-__host__ __device__ constexpr int at_smem_bytes(int tn, int ks, int stages) {
-  return pt_data_bytes(tn, ks, stages, 1) + at_low_bytes(tn, ks) + ((int)sizeof(AtTables) + 15) / 16 * 16 + (2 * PT_MAX_STAGES + 4) * 8;
-}
 
 template <bool Q8>
 __global__ void __launch_bounds__(AT_THREADS, 2)

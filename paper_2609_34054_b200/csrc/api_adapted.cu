@@ -137,53 +137,30 @@ struct Launch {
 
 template <int MT, int NT, bool Q8>
 int32_t launch_shrink(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
-  int ks = 8;                                    // blocks that share the K extent of a row tile
-  while (ks > 1 && (p.K / 64 < ks * SHRINK_WARPS || (p.M + 8LL * NT - 1) / (8 * NT) * ks > 2LL * ctx->sm_count)) ks >>= 1;
-  p.tile_rows = 8 * NT;
-  while (p.tile_rows > 1 && (p.M + p.tile_rows / 2 - 1LL) / (p.tile_rows / 2) * ks <= ctx->sm_count) p.tile_rows /= 2;
-  const long long tiles = (p.M + p.tile_rows - 1LL) / p.tile_rows;
-  Launch l(dim3((unsigned)(tiles * ks)), SHRINK_THREADS, 0, ks, stream);
+  const ShrinkPlan plan = plan_shrink(p.M, p.K, 8 * NT, ctx->sm_count);
+  p.tile_rows = plan.rows;
+  Launch l(dim3((unsigned)((p.M + plan.rows - 1LL) / plan.rows * plan.ks)), SHRINK_THREADS, 0, plan.ks, stream);
   PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_shrink_kernel<MT, NT, Q8>, p));
   return PRECC_OK;
 }
-int env_int(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 0; }
 
 template <bool Q8>
-int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, int smem_free, cudaStream_t stream) {
-  const int nkb = p.K / (Q8 ? 128 : 64);
-  const int rounds = (p.M + ctx->sm_count * 256 - 1) / (ctx->sm_count * 256);
-  p.BN = ((p.M + ctx->sm_count * rounds - 1) / (ctx->sm_count * rounds) + 15) / 16 * 16;
-  int ks = 1;
-  if (env_int("AS_TN")) p.BN = env_int("AS_TN");
-  else if (p.M <= 4096) p.BN = std::max(p.BN, std::min(32, (p.M + 15) / 16 * 16));
-  const int tiles = (p.M + p.BN - 1) / p.BN;
-  while (ks < 8 && tiles * ks * 2 <= ctx->sm_count && nkb >= ks * 4) ks *= 2;
-  const int slots = AS_LANES / p.rank, chunks = std::min(AS_CHUNKS<Q8>, (p.n_agents + slots - 1) / slots);
-  p.tmem_cols = 32;
-  while (p.tmem_cols < std::min(chunks * p.BN, 512)) p.tmem_cols <<= 1;
-  // behind the ring: 64 rows of an accumulator, and the sums of a K slice
-  const int tail = AS_TAIL_BYTES + (ks > 1 ? p.BN * p.rank * 4 : 0), most = ctx->max_smem_optin - 4096 - tail;
-  p.kps = 4;                                     // k-blocks in a slot: as many as leave three slots and every block two of them to do
-  if (env_int("AS_KPS")) p.kps = env_int("AS_KPS");
-  const int typical = p.BN * AP_ROW_BYTES + std::min(p.n_agents, 2) * p.rank * AP_ROW_BYTES * (Q8 ? 2 : 1);
-  const int whole = p.BN * AP_ROW_BYTES + AS_CHUNK_BYTES<Q8>;                // with all lanes of one accumulator: 64 KB at most, beside a tail of up to 97 KB
-  while (p.kps > 1 && (3 * p.kps * typical > most || p.kps * whole > most || nkb < 2 * ks * p.kps)) p.kps /= 2;
-  const int slot = p.kps * whole;
-  const int ring = std::min(most, std::max(smem_free, 3 * slot));
-  const int smem = ring + tail + 1024;
+int32_t launch_shrink_tc(precc_ctx* ctx, AdaptedParams p, cudaStream_t stream) {
+  const ShrinkTcPlan plan = plan_shrink_tc(p.M, p.K / (Q8 ? 128 : 64), p.rank, p.n_agents, Q8, ctx->sm_count, ctx->max_smem_optin);
+  p.BN = plan.tn; p.kps = plan.kps; p.tmem_cols = plan.tmem_cols;
   CUtensorMap map_x, map_a;
   int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, p.BN, Q8, p.kps);
   if (!rc) rc = map_weights(ctx, &map_a, p.A, p.n_agents * p.rank * (Q8 ? 2 : 1), p.K, p.rank, Q8);
   if (rc) return rc;
-  PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_shrink_tc_kernel<Q8>, smem));
-  Launch l(dim3((unsigned)ks, (unsigned)tiles), AS_THREADS, smem, ks, stream);
-  PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_shrink_tc_kernel<Q8>, map_x, map_a, p, ring));
+  PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_shrink_tc_kernel<Q8>, plan.smem));
+  Launch l(dim3((unsigned)((p.M + (long long)p.BN - 1) / p.BN * plan.ks)), AS_THREADS, plan.smem, plan.ks, stream);
+  PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_shrink_tc_kernel<Q8>, map_x, map_a, p, plan.ring));
   return PRECC_OK;
 }
 
 template <bool Q8>
 int32_t run_shrink(precc_ctx* ctx, const AdaptedParams& p, bool tc, cudaStream_t stream) {
-  if (tc) return launch_shrink_tc<Q8>(ctx, p, env_int("AS_SMEM") ? env_int("AS_SMEM") : 1 << 20, stream);
+  if (tc) return launch_shrink_tc<Q8>(ctx, p, stream);
   const bool few = p.M <= 64;
   switch (p.rank_pad) {
     case 16: return few ? launch_shrink<1, 1, Q8>(ctx, p, stream) : launch_shrink<1, 4, Q8>(ctx, p, stream);
@@ -192,22 +169,11 @@ int32_t run_shrink(precc_ctx* ctx, const AdaptedParams& p, bool tc, cudaStream_t
   }
 }
 
-constexpr int SHRINK_SMEM = 38 * 1024;           // what a block of the shrink kernel takes at most: left free beside the main kernel
-
 template <bool Q8>
-int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, bool beside_shrink, cudaStream_t stream) {
-  const int m_tiles = (p.M + AP_BM - 1) / AP_BM, pairs_max = ctx->sm_count / 2;
-  double best = 1e30;
-  for (int bn : {256, 192, 128, 64}) {
-    const long long tiles = (long long)m_tiles * ((p.N + bn - 1) / bn);
-    const double cost = (double)((tiles + pairs_max - 1) / pairs_max) * (bn + 40);
-    if (cost < best - 1e-9) { best = cost; p.BN = bn; }
-  }
-  const int stage = ap_stage_bytes(p.BN);
-  p.stages = std::min(AP_MAX_STAGES, (ctx->max_smem_optin - 4096 - (beside_shrink ? SHRINK_SMEM : 0)) / stage);
+int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, const AdaptedPlan& plan, cudaStream_t stream) {
+  p.BN = plan.bn; p.stages = plan.stages;
   p.tmem_cols = 32;
   while (p.tmem_cols < 2 * p.BN) p.tmem_cols <<= 1;
-  const int smem = p.stages * stage + (2 * p.stages + 6) * 8 + 1024;
   CUtensorMap map_x, map_w, map_t, map_b;
   int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, GEMM_BM, Q8);
   if (!rc) rc = map_weights(ctx, &map_w, W, p.N, p.K, p.BN / 2, Q8);
@@ -218,9 +184,10 @@ int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, bool beside_shr
     map_t = map_b = map_x;
   }
   if (rc) return rc;
-  const long long tiles = (long long)m_tiles * ((p.N + p.BN - 1) / p.BN);
+  const long long tiles = (p.M + AP_BM - 1LL) / AP_BM * ((p.N + p.BN - 1) / p.BN);
+  const int smem = ap_smem_bytes(p.BN, p.stages);
   PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_pair_kernel<Q8>, smem));
-  Launch l(dim3((unsigned)(2 * std::min<long long>(tiles, pairs_max))), AP_THREADS, smem, 2, stream);
+  Launch l(dim3((unsigned)(2 * std::min<long long>(tiles, ctx->sm_count / 2))), AP_THREADS, smem, 2, stream);
   PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_pair_kernel<Q8>, map_x, map_w, map_t, map_b, p));
   return PRECC_OK;
 }
@@ -235,53 +202,24 @@ int32_t launch_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaSt
 }
 template <bool Q8>
 int32_t run_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaStream_t stream) {
-  static const int force = getenv("AF_MT") ? atoi(getenv("AF_MT")) : 0;
-  const bool wide = force ? force == 2 : p.N > 16 * 4 * ctx->sm_count;
+  // sixteen columns a block, two blocks a SM, until that makes more than two waves; then 32 columns, whose blocks read X half as often
+  const bool wide = p.N > 16 * 4 * ctx->sm_count;
   if (p.M <= 8) return wide ? launch_few<1, 2, Q8>(ctx, p, W, stream) : launch_few<1, 1, Q8>(ctx, p, W, stream);
   return wide ? launch_few<2, 2, Q8>(ctx, p, W, stream) : launch_few<2, 1, Q8>(ctx, p, W, stream);
 }
 
 template <bool Q8>
-int32_t run_turn(precc_ctx* ctx, AdaptedParams p, const void* W, bool beside_shrink, cudaStream_t stream) {
-  const int nkb = p.K / (Q8 ? 128 : 64);
-  const int* fit = turn_clusters(ctx);
-  const int limit = ctx->max_smem_optin - (beside_shrink ? SHRINK_SMEM : 0);
-  const int groups = (p.N + PT_COLS - 1) / PT_COLS;
-  const int f_tn = env_int("AT_TN"), f_ks = env_int("AT_KS");
-  int best_tn = 0, best_ks = 0, best_st = 0;
-  double best = 1e30;
-  for (int t = (p.M + PT_MAX_TN - 1) / PT_MAX_TN, last = 0; t <= p.M; ++t) {
-    int tn = ((p.M + t - 1) / t + 15) / 16 * 16;
-    if (f_tn) tn = f_tn;
-    if (tn == last) { if (tn == 16) break; else continue; }
-    last = tn;
-    const long long tiles = (p.M + tn - 1) / tn;
-    for (int ks = 1; ks <= GEMM_MAX_KS && ks <= nkb; ++ks) {          // (every block of a cluster has a step)
-      if (f_ks && ks != f_ks) continue;
-      const int resident = ks == 1 ? ctx->sm_count : fit[ks];
-      if (resident < 1) continue;
-      const long long waves = (groups * tiles + resident - 1) / resident;
-      const int kb = (nkb + ks - 1) / ks;
-      int st = std::min(kb, PT_MAX_STAGES);
-      while (st > 0 && at_smem_bytes(tn, ks, st) > limit) --st;
-      if (st < std::min(kb, 3)) continue;
-      const double cost = waves * (1.5 + kb * (0.37 + 0.00036 * tn) + 0.005 * pt_share(tn, ks) * (ks - 1) + 0.0113 * tn + 0.1 * ks);
-      if (cost < best) { best = cost; best_tn = tn; best_ks = ks; best_st = st; }
-    }
-    if (f_tn || tn == 16) break;
-  }
-  if (best_ks == 0) return fail(ctx, PRECC_ERR_UNSUPPORTED, "no plan");
-  p.BN = best_tn; p.stages = best_st;
+int32_t run_turn(precc_ctx* ctx, AdaptedParams p, const void* W, const AdaptedPlan& plan, cudaStream_t stream) {
+  p.BN = plan.tn; p.stages = plan.stages;
   p.tmem_cols = 32;
   while (p.tmem_cols < p.BN) p.tmem_cols <<= 1;
-  if (getenv("AT_SHOW")) fprintf(stderr, "turn M %d N %d K %d: tn %d ks %d st %d cost %.2f\n", p.M, p.N, p.K, best_tn, best_ks, best_st, best);
-  const int smem = std::max(PT_MIN_SMEM, at_smem_bytes(p.BN, best_ks, p.stages));
+  const int smem = std::max(PT_MIN_SMEM, at_smem_bytes(p.BN, plan.ks, p.stages));
   CUtensorMap map_x, map_w;
   int32_t rc = map_rows(ctx, &map_x, p.x, p.M, p.K, p.BN, Q8);
   if (!rc) rc = map_weights(ctx, &map_w, W, p.N, p.K, PT_COLS, Q8);
   if (rc) return rc;
   PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_turn_kernel<Q8>, smem));
-  Launch l(dim3((unsigned)best_ks, (unsigned)groups, (unsigned)((p.M + p.BN - 1) / p.BN)), AT_THREADS, smem, best_ks, stream);
+  Launch l(dim3((unsigned)plan.ks, (unsigned)((p.N + PT_COLS - 1) / PT_COLS), (unsigned)((p.M + p.BN - 1) / p.BN)), AT_THREADS, smem, plan.ks, stream);
   PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_turn_kernel<Q8>, map_x, map_w, p));
   return PRECC_OK;
 }
@@ -323,16 +261,17 @@ int32_t project(precc_ctx* ctx, const precc_projection* d, const void* X, const 
   rc = check_device(ctx);
   if (rc) return rc;
   cudaStream_t st = (cudaStream_t)stream;
-  const bool tc = adapters && (env_int("AS_TC") ? M >= env_int("AS_TC") : M >= 2048);
+  const AdaptedPlan plan = plan_adapted(M, p.N, p.K, adapters ? p.rank : 0, Q8, ctx->sm_count, ctx->max_smem_optin, turn_clusters(ctx), ctx->adapted_kernel,
+                                        ctx->adapted_shrink);
   if (adapters) {
-    rc = run_shrink<Q8>(ctx, p, tc, st);
+    rc = run_shrink<Q8>(ctx, p, plan.shrink_tc, st);
     if (rc) return rc;
   }
-  const bool beside = adapters && !tc;
-  const int kind = env_int("AP_KIND"), turn_max = env_int("AP_TURN_MAX") ? env_int("AP_TURN_MAX") : 1024;
-  if ((M <= AF_MAX_ROWS && kind == 0) || kind == 1) return run_few<Q8>(ctx, p, W, st);
-  if ((M <= turn_max && kind == 0) || kind == 2) return run_turn<Q8>(ctx, p, W, beside, st);
-  return run_pair<Q8>(ctx, p, W, beside, st);
+  switch (plan.kernel) {
+    case ADAPTED_FEW: return run_few<Q8>(ctx, p, W, st);
+    case ADAPTED_TURN: return run_turn<Q8>(ctx, p, W, plan, st);
+    default: return run_pair<Q8>(ctx, p, W, plan, st);
+  }
 }
 
 }  // namespace

@@ -230,6 +230,8 @@ int32_t precc_create(precc_ctx** out, int32_t device) {
   if (const char* v = getenv("PRECC_PREFILL_VHALF")) ctx->no_prefill_vhalf = (strcmp(v, "0") == 0);
   if (const char* v = getenv("PRECC_PREFILL_HELPERS")) ctx->no_prefill_helpers = (strcmp(v, "0") == 0);
   if (const char* v = getenv("PRECC_PREFILL_HELPER_P")) ctx->prefill_helper_p = atoi(v);
+  if (const char* v = getenv("PRECC_ADAPTED")) ctx->adapted_kernel = strcmp(v, "few") == 0 ? 1 : strcmp(v, "turn") == 0 ? 2 : strcmp(v, "pair") == 0 ? 3 : 0;
+  if (const char* v = getenv("PRECC_ADAPTED_SHRINK")) ctx->adapted_shrink = strcmp(v, "mma") == 0 ? 1 : strcmp(v, "tc") == 0 ? 2 : 0;
   if (const char* v = getenv("PRECC_PREFILL_HELPER_MIN")) { const int n = atoi(v); if (n >= 8) ctx->prefill_helper_min_steps = n; }
   if (e != cudaSuccess) {
     fprintf(stderr, "precc_create: %s\n", cudaGetErrorString(e));

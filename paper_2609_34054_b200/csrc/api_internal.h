@@ -42,6 +42,8 @@ struct precc_ctx {
   bool no_prefill_vhalf = false;       // PRECC_PREFILL_VHALF=0 in the environment: the value ring of the tcgen05 prefill kernel always holds whole steps
   bool no_prefill_helpers = false;     // PRECC_PREFILL_HELPERS=0 in the environment: prefill with a workspace never uses helper blocks
   int prefill_helper_p = 0;            // PRECC_PREFILL_HELPER_P=n in the environment: the tiles' own blocks stop after n steps (experiments; 0 = planner's choice)
+  int adapted_kernel = 0;              // PRECC_ADAPTED=few|turn|pair in the environment: main kernel of the adapted projection where it can take the call (tests, experiments)
+  int adapted_shrink = 0;              // PRECC_ADAPTED_SHRINK=mma|tc in the environment: which kernel takes its rank-r product
   int prefill_helper_min_steps = 48;   // PRECC_PREFILL_HELPER_MIN=n in the environment: shortest context (128-token steps) that gets helper blocks
   char err[512] = {0};
   CUresult (*encode_tiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,

@@ -6,6 +6,26 @@ using namespace precc;
 
 namespace {
 
+// Pieces of eight columns per thread (c), threads of a row, and whether several rows share a block.
+// One row or a few: a piece a thread, for latency (1 x 4096: 2.3 us, 2.6 with two, 3.0 with four).  Many rows: what a thread has asked for at once has to cover the
+// latency of memory, 64 bytes - two pieces with their residual, or four without.  32768 x 4096, 8-bit output, us with one / two / four pieces: with the
+// residual 187 / 136 / 137, without 180 / 121 / 106 (16384 x 8192 with it: 239 / 144 / 136;
+// 1337 x 3584 without 9.0 / 7.4 / 8.8; eight pieces are slower everywhere).  Many short rows: a warp each, as blocks of one or two
+// warps are bound by how fast blocks start (30000 x 512: 32 us in blocks of 64 threads).
+struct NormPlan { int c, threads; bool shared_block; };
+NormPlan plan_norm(int rows, int pieces, bool residual) {
+  auto whole_warps = [&](int c) { return ((pieces + c - 1) / c + 31) / 32 * 32; };
+  if (pieces <= 32) {
+    int t = 1;
+    while (t < pieces) t *= 2;
+    return {1, t, true};
+  }
+  if (rows > 1024 && pieces <= 128) return {pieces <= 64 ? 2 : 4, 32, true};
+  int c = rows <= 148 ? 1 : (residual ? pieces <= 512 : rows <= 4096) ? 2 : 4;
+  if (c == 1 && whole_warps(1) > 1024) c = 4;
+  return {c, whole_warps(c), false};
+}
+
 template <int C, bool SHORT>
 int32_t norm_launch(precc_ctx* ctx, const NormParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
@@ -44,13 +64,8 @@ extern "C" int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* res
   p.residual_out = (__nv_bfloat16*)residual_out; p.out = (__nv_bfloat16*)out; p.q = (uint8_t*)out_e4m3; p.q_scale = out_scale;
   p.rows = rows; p.pieces = width / 8; p.inv_width = 1.0f / width; p.eps = eps;
   cudaStream_t st = (cudaStream_t)stream;
-  if (p.pieces <= 32) {
-    p.T = 1;
-    while (p.T < p.pieces) p.T *= 2;
-    return norm_launch<1, true>(ctx, p, st);
-  }
-  auto threads = [&](int c) { return ((p.pieces + c - 1) / c + 31) / 32 * 32; };
-  if (threads(1) <= 1024) { p.T = threads(1); return norm_launch<1, false>(ctx, p, st); }
-  p.T = threads(4);
-  return norm_launch<4, false>(ctx, p, st);
+  const NormPlan plan = plan_norm(rows, p.pieces, residual != nullptr);
+  p.T = plan.threads;
+  if (plan.shared_block) return plan.c == 1 ? norm_launch<1, true>(ctx, p, st) : plan.c == 2 ? norm_launch<2, true>(ctx, p, st) : norm_launch<4, true>(ctx, p, st);
+  return plan.c == 1 ? norm_launch<1, false>(ctx, p, st) : plan.c == 2 ? norm_launch<2, false>(ctx, p, st) : norm_launch<4, false>(ctx, p, st);
 }

@@ -1,6 +1,7 @@
 """precc_adapted_project / _e4m3 against the definition in 64 bits: one row to thousands, odd sizes, every rank, agents in runs and row by row,
 rows without an adapter, adapters and rows that hold NaN, packing, captured calls, and what is refused."""
 import math
+import os
 
 import pytest
 import torch
@@ -15,6 +16,22 @@ E4M3 = torch.float8_e4m3fn
 @pytest.fixture(scope="module")
 def px():
     p = Precc(0)
+    yield p
+    torch.cuda.synchronize()
+    assert p.poll_status() == 0
+    p.close()
+
+
+@pytest.fixture(scope="module", params=[("turn", "mma"), ("turn", "tc"), ("pair", "mma"), ("pair", "tc"), ("few", "tc")], ids="-".join)
+def forced(request):
+    """A context that takes one pair of kernels wherever they can take the call."""
+    old = {k: os.environ.get(k) for k in ("PRECC_ADAPTED", "PRECC_ADAPTED_SHRINK")}
+    os.environ["PRECC_ADAPTED"], os.environ["PRECC_ADAPTED_SHRINK"] = request.param
+    try:
+        p = Precc(0)
+    finally:
+        for k, v in old.items():
+            os.environ.pop(k) if v is None else os.environ.__setitem__(k, v)
     yield p
     torch.cuda.synchronize()
     assert p.poll_status() == 0
@@ -128,6 +145,20 @@ def test_64_agents(px, rows, rank, e4m3):
     _run(px, rows, 512, 328, rank, 64, "rows", e4m3)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rank", [0, 8, 16, 32, 64])
+@pytest.mark.parametrize("rows,k,n", [(1, 128, 40), (16, 1024, 520), (17, 256, 136), (64, 512, 64), (129, 2048, 128), (300, 384, 1000), (1500, 256, 264), (4097, 640, 72)])
+def test_every_kernel_takes_every_size(forced, rows, k, n, rank, e4m3):
+    _run(forced, rows, k, n, rank, 5, "rows", e4m3, seed=rank)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rank", [8, 64])
+@pytest.mark.parametrize("rows", [3, 100, 700])
+def test_every_kernel_takes_64_agents(forced, rows, rank, e4m3):
+    _run(forced, rows, 512, 328, rank, 64, "rows", e4m3)
+
+
 @pytest.mark.parametrize("rows", [4, 50, 200, 1000])
 def test_the_largest_width_and_depth(px, rows):
     _run(px, rows, 14336, 4096, 32, 3, "rows", False)
@@ -137,6 +168,16 @@ def test_the_largest_width_and_depth(px, rows):
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("rows", [1, 6, 24, 70, 150, 400, 1300, 2600])
 def test_other_adapters_and_rows_do_not_reach_a_row(px, rows, e4m3):
+    _isolation(px, rows, e4m3)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows", [6, 70, 400])
+def test_no_kernel_lets_other_adapters_reach_a_row(forced, rows, e4m3):
+    _isolation(forced, rows, e4m3)
+
+
+def _isolation(px, rows, e4m3):
     """Bit for bit the same whatever the other agents' adapters and the other rows hold, infinities and NaN among them."""
     k, n, r, agents = 512, 264, 16, 6
     x, w, A, B = _draw(k, n, r, agents, rows, seed=3)

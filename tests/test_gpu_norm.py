@@ -53,7 +53,7 @@ def _check(x, r, g, out, res_out, q, scale, eps=EPS):
 
 
 @pytest.mark.parametrize("width", [8, 16, 24, 64, 120, 128, 256, 264, 1000, 2048, 3584, 4096, 8192, 8200, 16384, 32768])
-@pytest.mark.parametrize("rows", [1, 3, 37, 700])
+@pytest.mark.parametrize("rows", [1, 3, 37, 700, 2001])
 def test_norm_matches_the_definition(px, rows, width):
     x, r, g = _inputs(rows, width, seed=width + rows)
     out, res_out = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
@@ -64,12 +64,13 @@ def test_norm_matches_the_definition(px, rows, width):
 
 @pytest.mark.parametrize("residual", [False, True])
 @pytest.mark.parametrize("outputs", ["bf16", "e4m3"])
-@pytest.mark.parametrize("width", [128, 4096, 16000])
-def test_norm_forms(px, width, outputs, residual):
-    x, r, g = _inputs(301, width, seed=5, residual=residual)
+@pytest.mark.parametrize("width", [128, 520, 4096, 16000])
+@pytest.mark.parametrize("rows", [301, 5003])
+def test_norm_forms(px, rows, width, outputs, residual):
+    x, r, g = _inputs(rows, width, seed=5, residual=residual)
     out = torch.empty_like(x) if outputs == "bf16" else None
     q = torch.empty(x.shape, dtype=E4M3, device="cuda") if outputs == "e4m3" else None
-    scale = torch.empty(301, device="cuda") if outputs == "e4m3" else None
+    scale = torch.empty(rows, device="cuda") if outputs == "e4m3" else None
     px.rms_norm(x, g, EPS, out=out, residual=r, out_e4m3=q, out_scale=scale)
     _check(x, r, g, out, None, q, scale)
 
