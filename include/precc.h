@@ -225,8 +225,9 @@ int32_t precc_workspace_init(precc_ctx* ctx, void* workspace, size_t workspace_b
  * A request whose ctx_len exceeds max_ctx is rejected on the device: zeros, PRECC_STATUS_BAD_INDEX.
  * B == 0 is a no-op.
  * Overlap with the kernel before it on the stream.  The launch is a programmatic dependent launch: where the
- * preceding kernel permits it (of this library: another decode or combine launch, and the few-row projection
- * that serves calls of at most 64 rows; kernels of other libraries normally do not) the decode kernel starts
+ * preceding kernel permits it (of this library: another decode or combine launch, the few-row projection
+ * that serves calls of at most 64 rows, and the norm and the adapted projections, which permit it once everything
+ * before them has completed; kernels of other libraries normally do not) the decode kernel starts
  * while that kernel still runs and, before it waits for it to finish, already reads ctx_len, agent_id, the block
  * table / first_block, B_k, B_v and every cache page that holds none of the request's last 64 tokens (logical
  * positions ctx_len-64 .. ctx_len-1).  q, the pages holding those last 64 tokens and every store come after the

@@ -123,6 +123,23 @@ def layer_weights(geo: Geometry, seed: int, tag: str = "L0") -> Dict[str, torch.
     return out
 
 
+def block_weights(geo: Geometry, seed: int, tag: str = "L0") -> Dict[str, torch.Tensor]:
+    """Query and output projections of one layer, all agents' adapters on them (rank of the value side), and the norm's gain.
+
+    W ~ N(0, 0.02^2); A ~ N(0, 1/d_in); B ~ N(0, 0.02^2); gain ~ 1 + N(0, 0.1^2).
+    """
+    d, w, n, r = geo.d_model, geo.n_q * geo.hd, geo.n_agents, geo.rank_v
+    return {
+        "W_q": normal_bf16((d, w), 0.02, seed, f"{tag}.W_q"),
+        "W_o": normal_bf16((w, d), 0.02, seed, f"{tag}.W_o"),
+        "A_q": normal_bf16((n, d, r), d ** -0.5, seed, f"{tag}.A_q"),
+        "B_q": normal_bf16((n, r, w), 0.02, seed, f"{tag}.B_q"),
+        "A_o": normal_bf16((n, w, r), w ** -0.5, seed, f"{tag}.A_o"),
+        "B_o": normal_bf16((n, r, d), 0.02, seed, f"{tag}.B_o"),
+        "gain": (1 + normal_bf16((d,), 0.1, seed, f"{tag}.gain").float()).to(torch.bfloat16),
+    }
+
+
 def hidden_states(n_tokens: int, geo: Geometry, seed: int, tag: str = "L0.H") -> torch.Tensor:
     """Hidden states H ~ N(0,1), [n_tokens, d]."""
     return normal_bf16((n_tokens, geo.d_model), 1.0, seed, tag)

@@ -3,7 +3,7 @@
 A trace is a list of agent turns over one growing shared trajectory: turn = (agent j, n_in tokens that
 arrive as input, n_out tokens the agent decodes).  For every layer the replay issues exactly the KV-path
 work a sharing policy implies and nothing else (no MLP, no query/output projections, random hidden
-states and queries), so its times are the KV-path share of a turn, not model latencies:
+states and queries), so its times are the KV-path share of a turn, not model latencies (``block`` below adds the rest of the attention):
 
   prelr       PreLRShared: new tokens -> base rows + LR rows of ALL agents (one fused projection), then
               attention of agent j over base + own LR cache; the same per decoded token.
@@ -26,7 +26,11 @@ TTFT of a turn = its prefill phase (projection + prefill attention over all laye
 the sum over turns; throughput = trajectory tokens / total time (Section 4.1).  Decode steps are one
 CUDA graph per turn (all layers, device-side context length and slot), replayed n_out times.
 
-Run:  python -m paper_2609_34054_b200.replay --lengths 1900,17300,66400 --layers 32
+With ``block`` ("bf16" or "e4m3") a layer is a whole attention block (block.py): the residual stream is normed, projected to queries with
+the agent's adapters, and the attention's output projected back, so that every layer sees the hidden states that the one before it left;
+the adapted and the adapter-free sequence of double batching are then rows of one batch with an agent each.
+
+Run:  python -m paper_2609_34054_b200.replay --lengths 1900,17300,66400 --layers 32 [--block e4m3]
 """
 from __future__ import annotations
 
@@ -39,6 +43,7 @@ import torch
 
 from . import inputs as I
 from .binding import Cache, Precc, layer_desc
+from .block import AttentionBlocks
 
 POLICIES = ("prelr", "rebase_lp", "rebase_db", "fullshared", "nonshared")
 
@@ -81,7 +86,7 @@ class Stack:
     and outputs a function of the trace that a test can recompute)."""
 
     def __init__(self, px: Precc, geo: I.Geometry, n_layers: int, max_tokens: int, max_rows: int, seed: int = 0,
-                 shared_weights: bool = False, private_tokens: int = 0):
+                 shared_weights: bool = False, private_tokens: int = 0, block: str = ""):
         self.px, self.geo, self.n_layers = px, geo, n_layers
         self.desc = layer_desc(geo)
         n_blocks = (max_tokens + I.PAGE - 1) // I.PAGE
@@ -107,6 +112,9 @@ class Stack:
         self.out = torch.empty_like(self.q)
         self.ws = px.decode_workspace(self.desc, 2, max_tokens)      # up to two requests per launch (double batching)
         self.max_tokens = max_tokens
+        if block not in ("", "bf16", "e4m3"):
+            raise ValueError("block must be empty, 'bf16' or 'e4m3'")
+        self.blocks = AttentionBlocks(px, geo, n_layers, max(max_rows, 2), seed, shared_weights, block == "e4m3") if block else None
 
     def w(self, l: int) -> int:
         return l if len(self.WA) > 1 else 0
@@ -124,6 +132,13 @@ def _project(st: Stack, l: int, H: torch.Tensor, start: int, mask: Optional[int]
 def _prefill_phase(st: Stack, H: torch.Tensor, T: int, agent: int, mask: Optional[int]):
     """The n = len(H) tokens at positions T.. : projection into the caches, then attention of `agent` over them."""
     n = H.shape[0]
+    if st.blocks:
+        def attend(l, h, q, out):
+            _project(st, l, h, T, mask)
+            k = st.w(l)
+            st.px.lr_attend_prefill(st.desc, q, agent, T, st.B_k[k], st.B_v[k], st.caches[l], out)
+        st.blocks.forward(H, torch.full((n,), agent, dtype=torch.int32, device=H.device), attend)
+        return
     for l in range(st.n_layers):
         _project(st, l, H, T, mask)
         k = st.w(l)
@@ -144,11 +159,17 @@ class _DecodeGraph:
 
         def step():
             torch.index_select(H_src, 0, self.pos, out=st.stage[:1])
-            for l in range(st.n_layers):
-                _project(st, l, st.stage[:1], 0, mask, self.slot)
+
+            def layer(l, h, q, out):
+                _project(st, l, h, 0, mask, self.slot)
                 k = st.w(l)
-                st.px.lr_attend_decode(st.desc, st.q[:1], self.agent, self.ctx, max_ctx, st.B_k[k], st.B_v[k], st.caches[l],
-                                       st.out[:1], st.ws, None, self.first)
+                st.px.lr_attend_decode(st.desc, q, self.agent, self.ctx, max_ctx, st.B_k[k], st.B_v[k], st.caches[l],
+                                       out, st.ws, None, self.first)
+            if st.blocks:
+                st.blocks.forward(st.stage[:1], self.agent, layer)
+            else:
+                for l in range(st.n_layers):
+                    layer(l, st.stage[:1], st.q[:1], st.out[:1])
             self.ctx.add_(1)
             self.slot.add_(1)
             self.pos.add_(1)
@@ -206,7 +227,7 @@ def _replay_db(st: Stack, turns: Sequence[Turn]) -> Dict[str, float]:
         st.H2[n:2 * n].copy_(st.H_neut[P:P + n])
 
         def prefill_both():
-            for l in range(st.n_layers):
+            def layer(l, h, q, out):
                 k = st.w(l)
                 if P % I.PAGE:
                     # the page that holds position P is private to the adapted sequence: it starts as a copy of the
@@ -218,9 +239,14 @@ def _replay_db(st: Stack, turns: Sequence[Turn]) -> Dict[str, float]:
                     if c.lr_v is not None:
                         c.lr_v[:, dst].copy_(c.lr_v[:, src])
                 # adapted rows and adapter-free rows of the turn in ONE projection (per-row agent masks)
-                px.turn_project_rows(st.desc, st.H2[:2 * n], st.WA[k], st.caches[l], slots_2n, masks_2n, copy_2n)
-                px.lr_attend_prefill(st.desc, st.q[:n], j, P, st.B_k[k], st.B_v[k], st.caches[l], st.out[:n], table_a)
-                px.lr_attend_prefill(st.desc, st.q[:n], -1, P, st.B_k[k], st.B_v[k], st.caches[l], st.out[:n])
+                px.turn_project_rows(st.desc, h, st.WA[k], st.caches[l], slots_2n, masks_2n, copy_2n)
+                px.lr_attend_prefill(st.desc, q[:n], j, P, st.B_k[k], st.B_v[k], st.caches[l], out[:n], table_a)
+                px.lr_attend_prefill(st.desc, q[-n:], -1, P, st.B_k[k], st.B_v[k], st.caches[l], out[-n:])
+            if st.blocks:
+                st.blocks.forward(st.H2[:2 * n], torch.tensor([j] * n + [-1] * n, dtype=torch.int32, device=dev), layer)
+            else:
+                for l in range(st.n_layers):
+                    layer(l, st.H2[:2 * n], st.q[:n], st.out[:n])
 
         ttft += _timed(prefill_both)
         if t.n_out > 0:
@@ -240,11 +266,16 @@ def _replay_db(st: Stack, turns: Sequence[Turn]) -> Dict[str, float]:
             def step():
                 torch.index_select(st.H_adpt, 0, pos, out=st.stage[:1])
                 torch.index_select(st.H_neut, 0, pos, out=st.stage[1:2])
-                for l in range(st.n_layers):
+
+                def layer(l, h, q, out):
                     k = st.w(l)
-                    px.turn_project_rows(st.desc, st.stage, st.WA[k], st.caches[l], slot2, mask2, copy2)
-                    px.lr_attend_decode(st.desc, st.q[:2], agent2, ctx, max_ctx, st.B_k[k], st.B_v[k], st.caches[l], st.out[:2],
-                                        st.ws, table2)
+                    px.turn_project_rows(st.desc, h, st.WA[k], st.caches[l], slot2, mask2, copy2)
+                    px.lr_attend_decode(st.desc, q, agent2, ctx, max_ctx, st.B_k[k], st.B_v[k], st.caches[l], out, st.ws, table2)
+                if st.blocks:
+                    st.blocks.forward(st.stage, agent2, layer)
+                else:
+                    for l in range(st.n_layers):
+                        layer(l, st.stage, st.q[:2], st.out[:2])
                 ctx.add_(1); slot2.add_(1); pos.add_(1); copy2[:1].add_(1)
 
             step()
@@ -310,6 +341,7 @@ def main(argv=None):
     ap.add_argument("--agents", type=int, default=3)
     ap.add_argument("--rank", type=int, default=32)
     ap.add_argument("--policies", default=",".join(POLICIES))
+    ap.add_argument("--block", default="", choices=("", "bf16", "e4m3"), help="whole attention blocks: norm, query and output projections too")
     ap.add_argument("--round-robin", type=int, default=0, help="instead of the length sweep: N agents, 8 turns x 8192 tokens")
     args = ap.parse_args(argv)
     px = Precc(0)
@@ -320,10 +352,10 @@ def main(argv=None):
     for turns in traces:
         total = trace_tokens(turns)
         rows = max(total, 64, 2 * max(t.n_in for t in turns))   # nonshared prefills nearly the whole trajectory at once; double batching 2 x n_in rows
-        st = Stack(px, geo, args.layers, total + I.PAGE, rows, private_tokens=max(t.n_in + t.n_out for t in turns) + I.PAGE)
+        st = Stack(px, geo, args.layers, total + I.PAGE, rows, private_tokens=max(t.n_in + t.n_out for t in turns) + I.PAGE, block=args.block)
         for pol in args.policies.split(","):
             r = replay(st, turns, pol)
-            r.update({"layers": args.layers, "n_agents": n_agents, "rank": args.rank})
+            r.update({"layers": args.layers, "n_agents": n_agents, "rank": args.rank, "block": args.block})
             print(json.dumps({k: (round(v, 3) if isinstance(v, float) else v) for k, v in r.items()}), flush=True)
         del st
         torch.cuda.empty_cache()
