@@ -1,11 +1,11 @@
-// The main kernel of the adapted projection for a handful of rows (decode steps, up to 16): one pass over the weights.
+// The main kernel of the adapted projection for a handful of rows (decode steps, up to 32): one pass over the weights.
 //
-// HBM-bound at K x N weights.  A block takes 16 MT output columns over the whole K extent, its eight warps every eighth k-block
+// HBM-bound at K x N weights.  A block takes 16 output columns over the whole K extent, its eight warps every eighth k-block
 // (so nothing is merged between blocks), and each warp asks for several k-blocks of weights before it uses the first: the
 // fragments of mma.sync come straight from the packed weights into registers, 16 bytes a lane, which keeps more of the matrix in
 // flight than a ring in shared memory would.  Output columns are the M axis of the MMA and the rows of X its N axis, so
 // eight rows cost nothing over one.
-// The adapters: warp u takes the u-th agent among the rows.  Its B slice (r x 16 MT) is asked for with the first weights and meets that agent's rows
+// The adapters: warp u takes the u-th agent among the rows.  Its B slice (r x 16) is asked for with the first weights and meets that agent's rows
 // of T once the shrink kernel is done; the rows of others are zero in the product and dropped from it.
 #pragma once
 #include "adapted.cuh"
@@ -22,20 +22,19 @@ __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   return v;
 }
 
-template <int NT, int MT>
-constexpr int AF_U = MT == 1 && NT == 2 ? 2 : 3;
+constexpr int AF_COLS = 16;                       // output columns of a block: the M axis of one MMA
 
-__host__ __device__ constexpr int af_smem_bytes(int nt, int mt, int rank_pad) {
-  return (AF_WARPS + 1) * 8 * nt * (16 * mt + 4) * 4 + AF_WARPS * rank_pad * (32 * mt + 16);
+__host__ __device__ constexpr int af_smem_bytes(int nt, int rank_pad) {
+  return (AF_WARPS + 1) * 8 * nt * (AF_COLS + 4) * 4 + AF_WARPS * rank_pad * (AF_COLS * 2 + 16);
 }
 
-// NT: eight-row pieces of X.  MT: sixteen-column pieces of a block.  Steps of 128 bytes of K (64 bf16, 128 e4m3).
-template <int NT, int MT, bool Q8>
-__global__ void __launch_bounds__(AF_THREADS, MT == 1 ? 2 : 1)
+// NT: eight-row pieces of X.  Steps of 128 bytes of K (64 bf16, 128 e4m3).
+template <int NT, bool Q8>
+__global__ void __launch_bounds__(AF_THREADS, NT < 4 ? 2 : 1)
 adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
-  constexpr int C = 16 * MT, S = C + 4;           // row of the partial sums, padded: the lanes of a store hit 32 banks
+  constexpr int C = AF_COLS, S = C + 4;           // row of the partial sums, padded: the lanes of a store hit 32 banks
   constexpr int BP = C * 2 + 16;                  // bytes of a row of a B slice, padded for ldmatrix
-  constexpr int U = AF_U<NT, MT>;                 // k-blocks of a warp in flight
+  constexpr int U = NT == 1 ? 3 : 2;              // k-blocks of a warp in flight: what the registers of two blocks a SM hold
   extern __shared__ __align__(16) uint8_t smem[];
   float (*red)[8 * NT][S] = reinterpret_cast<float (*)[8 * NT][S]>(smem);                    // [warp]
   float (*low)[S] = red[AF_WARPS];                                                           // s (x A) B of every row
@@ -48,22 +47,18 @@ adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
   const int nkb = p.K / (Q8 ? 128 : 64);
   const long long row_bytes = (long long)p.K * (Q8 ? 1 : 2);
   const uint8_t* x = static_cast<const uint8_t*>(p.x);
-  float acc[MT][NT][4];
+  float acc[NT][4];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n) { acc[m][n][0] = acc[m][n][1] = acc[m][n][2] = acc[m][n][3] = 0.f; }
-  uint4 wv[U][MT][2][2], xv[U][NT][2];            // [..][row g, row g + 8][piece t, piece t + 4]
+  for (int n = 0; n < NT; ++n) { acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f; }
+  uint4 wv[U][2][2], xv[U][NT][2];                // [..][row g, row g + 8][piece t, piece t + 4]
   auto fetch = [&](int u, int kb) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int h = 0; h < 2; ++h) {
+      const int n = n0 + h * 8 + g;
+      const uint4* src = reinterpret_cast<const uint4*>(W + ((long long)kb * p.N + n) * AP_ROW_BYTES);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int n = n0 + m * 16 + h * 8 + g;
-        const uint4* src = reinterpret_cast<const uint4*>(W + ((long long)kb * p.N + n) * AP_ROW_BYTES);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) wv[u][m][h][c] = kb < nkb && n < p.N ? ld_stream(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
-      }
+      for (int c = 0; c < 2; ++c) wv[u][h][c] = kb < nkb && n < p.N ? ld_stream(src + t + 4 * c) : make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const uint4* src = reinterpret_cast<const uint4*>(x + (n * 8 + g) * row_bytes + (long long)kb * AP_ROW_BYTES);
@@ -74,7 +69,7 @@ adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
 #pragma unroll
   for (int u = 0; u < U; ++u) fetch(u, warp + u * AF_WARPS);
 
-  // this warp's agents (the w-th and the w + 8-th among the rows), and their slices of B
+  // this warp's agents (every eighth among the rows, from the w-th on), and their slices of B
   int id = -1;
   if (adapters && lane < p.M) id = agent_of(p, lane);
   unsigned todo = __ballot_sync(0xffffffffu, id >= 0);
@@ -105,26 +100,22 @@ adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < 2; ++c) {
+        const uint32_t a0[4] = {wv[u][0][c].x, wv[u][1][c].x, wv[u][0][c].y, wv[u][1][c].y};
+        const uint32_t a1[4] = {wv[u][0][c].z, wv[u][1][c].z, wv[u][0][c].w, wv[u][1][c].w};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const uint32_t a0[4] = {wv[u][m][0][c].x, wv[u][m][1][c].x, wv[u][m][0][c].y, wv[u][m][1][c].y};
-          const uint32_t a1[4] = {wv[u][m][0][c].z, wv[u][m][1][c].z, wv[u][m][0][c].w, wv[u][m][1][c].w};
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            mma_step<Q8>(acc[m][n], a0, xv[u][n][c].x, xv[u][n][c].y);
-            mma_step<Q8>(acc[m][n], a1, xv[u][n][c].z, xv[u][n][c].w);
-          }
+        for (int n = 0; n < NT; ++n) {
+          mma_step<Q8>(acc[n], a0, xv[u][n][c].x, xv[u][n][c].y);
+          mma_step<Q8>(acc[n], a1, xv[u][n][c].z, xv[u][n][c].w);
         }
+      }
       fetch(u, kb + (u + U) * AF_WARPS);
     }
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) red[warp][n * 8 + 2 * t + (e & 1)][m * 16 + g + 8 * (e >> 1)] = acc[m][n][e];
+    for (int e = 0; e < 4; ++e) red[warp][n * 8 + 2 * t + (e & 1)][g + 8 * (e >> 1)] = acc[n][e];
 
   if (adapters) {
     pdl_wait();                                   // T is complete
@@ -135,32 +126,33 @@ adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
       if (i > 0) { __syncwarp(); fetch_b(agent[i]); }
       cp_async_wait<0>();
       __syncwarp();
-      float d[C / 8][4];
 #pragma unroll
-      for (int j = 0; j < C / 8; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
-      for (int k0 = 0; k0 < p.rank_pad; k0 += 16) {
-        uint32_t a[4];                            // rows g and g + 8 of T, coordinates 2t.. and 2t + 8..
+      for (int half = 0; half < (NT + 1) / 2; ++half) {          // sixteen rows at a time
+        if (!((mine[i] >> (16 * half)) & 0xffffu)) continue;
+        float d[C / 8][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int r = g + 8 * (q & 1);
-          const __nv_bfloat16* src = p.T + (long long)r * p.rank_pad + k0 + 2 * t + 8 * (q >> 1);
-          a[q] = (mine[i] >> r) & 1u ? *reinterpret_cast<const uint32_t*>(src) : 0u;
-        }
+        for (int j = 0; j < C / 8; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
+        for (int k0 = 0; k0 < p.rank_pad; k0 += 16) {
+          uint32_t a[4];                          // rows g and g + 8 of T, coordinates 2t.. and 2t + 8..
 #pragma unroll
-        for (int j = 0; j < C / 16; ++j) {
+          for (int q = 0; q < 4; ++q) {
+            const int r = 16 * half + g + 8 * (q & 1);
+            const __nv_bfloat16* src = p.T + (long long)r * p.rank_pad + k0 + 2 * t + 8 * (q >> 1);
+            a[q] = (mine[i] >> r) & 1u ? *reinterpret_cast<const uint32_t*>(src) : 0u;
+          }
           uint32_t b[4];                          // 16 coordinates x 16 columns
-          ldsm_x4_t(b, b_s + (k0 + (lane & 15)) * BP + j * 32 + (lane >> 4) * 16);
-          mma_bf16_16816(d[2 * j], a, b[0], b[1]);
-          mma_bf16_16816(d[2 * j + 1], a, b[2], b[3]);
+          ldsm_x4_t(b, b_s + (k0 + (lane & 15)) * BP + (lane >> 4) * 16);
+          mma_bf16_16816(d[0], a, b[0], b[1]);
+          mma_bf16_16816(d[1], a, b[2], b[3]);
         }
+#pragma unroll
+        for (int j = 0; j < C / 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 16 * half + g + 8 * (e >> 1);
+            if ((mine[i] >> r) & 1u) low[r][8 * j + 2 * t + (e & 1)] = d[j][e];
+          }
       }
-#pragma unroll
-      for (int j = 0; j < C / 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = g + 8 * (e >> 1);
-          if ((mine[i] >> r) & 1u) low[r][8 * j + 2 * t + (e & 1)] = d[j][e];
-        }
     }
   }
   __syncthreads();

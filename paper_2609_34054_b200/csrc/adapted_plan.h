@@ -11,8 +11,15 @@ namespace precc {
 constexpr int AP_MAX_AGENTS = 64;
 constexpr int AP_ROW_BYTES = 128;             // bytes of K in a k-block: 64 bf16 or 128 e4m3
 
-// ---- up to sixteen rows (adapted_few.cuh)
-constexpr int AF_MAX_ROWS = 16;
+// ---- few rows (adapted_few.cuh): up to sixteen with at most two waves of blocks of sixteen columns (two blocks an SM), up to 32, where a block holds an SM, with one;
+// past eight rows, where every step costs a warp more, none that its eight warps need more than eight steps for.  us, few / turn kernel, rank 16, bf16:
+// 8 rows, 4096 x 4096 10.7 / 13.9, 4096 x 9472 17.6 / 18.9, 8192 x 1024 9.1 / 11.0, but 4096 x 14336 24.5 / 22.3; 16 rows, 4096 x 4096 11.7 / 13.1,
+// 4096 x 9472 19.0 / 19.9, 2048 x 2048 6.5 / 9.0, but 7168 x 2048 14.8 / 12.7; 32 rows, 2048 x 2048 8.7 / 10.3, 3584 x 1280 10.9 / 11.4, but 4096 x 4096
+// 17.8 / 13.3 and 7168 x 2048 15.5 / 12.9.  In 8 bits the same, but for a second wave without adapters (8 rows, 4096 x 9472: 11.2 / 9.6).
+constexpr int AF_MAX_ROWS = 32;
+inline bool few_rows(int M, int K, int N, int sm_count) {
+  return M <= 8 ? N <= 64 * sm_count : M <= AF_MAX_ROWS && K <= 4096 && N <= (M <= 16 ? 64 : 16) * sm_count;
+}
 
 // ---- turns (adapted_turn.cuh)
 constexpr int AT_NO_ROW = 0xffff;
@@ -114,7 +121,7 @@ inline AdaptedPlan plan_adapted(int M, int N, int K, int rank, bool q8, int sm_c
   const int nkb = K / (q8 ? 128 : 64);
   r.shrink_tc = rank > 0 && (force_shrink ? force_shrink == 2 : shrink_on_tcgen05(M, rank, q8));
   const int limit = max_smem - (rank > 0 && !r.shrink_tc ? SHRINK_SMEM : 0);
-  if (M <= AF_MAX_ROWS && (force_kernel == 0 || force_kernel == ADAPTED_FEW)) { r.kernel = ADAPTED_FEW; return r; }
+  if (force_kernel == ADAPTED_FEW ? M <= AF_MAX_ROWS : force_kernel == 0 && few_rows(M, K, N, sm_count)) { r.kernel = ADAPTED_FEW; return r; }
   const PairPlan pair = plan_pair(M, N, nkb, sm_count);
   if (force_kernel != ADAPTED_PAIR && M <= 4096) {
     const AdaptedTurnPlan turn = plan_adapted_turn(M, N, nkb, sm_count, limit - 1024, clusters);

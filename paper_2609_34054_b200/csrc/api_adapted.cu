@@ -192,20 +192,17 @@ int32_t run_pair(precc_ctx* ctx, AdaptedParams p, const void* W, const AdaptedPl
   return PRECC_OK;
 }
 
-template <int NT, int MT, bool Q8>
+template <int NT, bool Q8>
 int32_t launch_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaStream_t stream) {
-  const int smem = af_smem_bytes(NT, MT, p.agent_id ? p.rank_pad : 0);
-  PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_few_kernel<NT, MT, Q8>, smem));
-  Launch l(dim3((unsigned)((p.N + 16 * MT - 1) / (16 * MT))), AF_THREADS, smem, 1, stream);
-  PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_few_kernel<NT, MT, Q8>, p, (const uint8_t*)W));
+  const int smem = af_smem_bytes(NT, p.agent_id ? p.rank_pad : 0);
+  PRECC_CUDA(ctx, raise_smem_limit(ctx, adapted_few_kernel<NT, Q8>, smem));
+  Launch l(dim3((unsigned)((p.N + AF_COLS - 1) / AF_COLS)), AF_THREADS, smem, 1, stream);
+  PRECC_CUDA(ctx, cudaLaunchKernelEx(&l.cfg, adapted_few_kernel<NT, Q8>, p, (const uint8_t*)W));
   return PRECC_OK;
 }
 template <bool Q8>
 int32_t run_few(precc_ctx* ctx, const AdaptedParams& p, const void* W, cudaStream_t stream) {
-  // sixteen columns a block, two blocks a SM, until that makes more than two waves; then 32 columns, whose blocks read X half as often
-  const bool wide = p.N > 16 * 4 * ctx->sm_count;
-  if (p.M <= 8) return wide ? launch_few<1, 2, Q8>(ctx, p, W, stream) : launch_few<1, 1, Q8>(ctx, p, W, stream);
-  return wide ? launch_few<2, 2, Q8>(ctx, p, W, stream) : launch_few<2, 1, Q8>(ctx, p, W, stream);
+  return p.M <= 8 ? launch_few<1, Q8>(ctx, p, W, stream) : p.M <= 16 ? launch_few<2, Q8>(ctx, p, W, stream) : launch_few<4, Q8>(ctx, p, W, stream);
 }
 
 template <bool Q8>

@@ -44,7 +44,7 @@ def test_every_call_has_a_kernel_that_fits(plan):
             what, nkb = (force, M, K, N, r, q), K // (128 if q else 64)
             limit = SMEM - (38 * 1024 if r and not tc else 0)
             if kernel == 1:
-                assert M <= 16 and not force, what
+                assert M <= 32 and N <= (64 if M <= 16 else 16) * SMS and (M <= 8 or K <= 4096) and not force, what
             elif kernel == 2:
                 assert 16 <= tn <= 256 and tn % 16 == 0 and 1 <= ks <= 8 and ks <= nkb and 1 <= stages <= 8, what
                 assert smem <= limit - 1024 and (M + tn - 1) // tn <= 65535 and (N + 127) // 128 <= 65535, what
