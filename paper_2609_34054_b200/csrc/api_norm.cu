@@ -22,7 +22,7 @@ NormPlan plan_norm(int rows, int pieces, bool residual) {
   }
   if (rows > 1024 && pieces <= 128) return {pieces <= 64 ? 2 : 4, 32, true};
   int c = rows <= 148 ? 1 : (residual ? pieces <= 512 : rows <= 4096) ? 2 : 4;
-  if (c == 1 && whole_warps(1) > 1024) c = 4;
+  if (whole_warps(c) > 1024) c = 4;
   return {c, whole_warps(c), false};
 }
 

@@ -75,6 +75,15 @@ def test_norm_forms(px, rows, width, outputs, residual):
     _check(x, r, g, out, None, q, scale)
 
 
+@pytest.mark.parametrize("width", [16384, 16392, 24000, 32768])
+@pytest.mark.parametrize("rows", [1, 148, 149, 300])
+def test_widest_rows_without_residual(px, rows, width):
+    x, _, g = _inputs(rows, width, seed=width, residual=False)
+    out = torch.full_like(x, float("nan"))
+    px.rms_norm(x, g, EPS, out=out)
+    _check(x, None, g, out, None, None, None)
+
+
 @pytest.mark.parametrize("width", [64, 4096])
 def test_norm_in_place(px, width):
     x, r, g = _inputs(65, width, seed=9)
