@@ -422,7 +422,7 @@ int32_t precc_combine_partials(precc_ctx* ctx, const precc_layer_desc* desc, con
  *                 scale of a row of zeros is 1; scales are not smaller than the least normal fp32.
  * Outputs may be x or residual themselves (the same address); other overlaps are not allowed.  A row with a NaN or an infinity is NaN
  * in that place of `out` or in all of it, has a NaN or infinite scale, and touches no other row.  The norm is of
- * the unrounded sum.  width: a multiple of 8, at most 32768.  rows == 0 is a no-op. */
+ * the unrounded sum, over the whole range of bf16.  width: a multiple of 8, at most 32768.  rows == 0 is a no-op. */
 int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, const void* gain, int32_t rows,
                        int32_t width, float eps, void* residual_out, void* out, void* out_e4m3,
                        float* out_scale, void* stream);
@@ -434,7 +434,8 @@ int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, cons
  *   A_packed    precc_pack_kmajor of every A_a [k_dim][rank], a = 0, 1, ..: dst_rows = n_agents*rank, dst_row0 = a*rank
  *   B           [n_agents][rank][n_out]
  *   agent_id    [M] in [-1, n_agents); NULL: no row has an adapter (A_packed, B and ws may be NULL then, as with
- *               rank 0).  A row with an id outside is computed without an adapter, and PRECC_STATUS_BAD_INDEX is recorded.
+ *               rank 0, where ids are not read).  A row with an id outside is computed without an adapter, and
+ *               PRECC_STATUS_BAD_INDEX is recorded.
  *   ws          device scratch of precc_adapted_ws_bytes(proj, M), 128-byte aligned, of any content; calls that may
  *               run at the same time (also from two captured graphs) need separate ones
  * X A is rounded to bf16 before it meets B; everything else is summed in fp32 and rounded once.  A row depends on its own row of

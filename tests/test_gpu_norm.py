@@ -117,7 +117,7 @@ def test_rows_of_zeros_and_non_finite_rows(px, width):
     x[1] = 0
     x[3, 5] = float("inf")
     x[5, 7] = float("nan")
-    x[7] = 1e30                                  # its squares overflow fp32: the root is infinite and y is 0
+    x[7] = 1e30
     out = torch.empty_like(x)
     q, scale = torch.empty(x.shape, dtype=E4M3, device="cuda"), torch.empty(9, device="cuda")
     px.rms_norm(x, g, EPS, out=out, out_e4m3=q, out_scale=scale)
@@ -126,6 +126,25 @@ def test_rows_of_zeros_and_non_finite_rows(px, width):
     assert (out[1] == 0).all() and (q[1].float() == 0).all() and scale[1] == 1
     assert torch.isnan(out[3, 5]) and not torch.isfinite(scale[3])
     assert torch.isnan(out[5]).all() and torch.isnan(scale[5]) and torch.isnan(q[5].float()).all()
+
+
+@pytest.mark.parametrize("rows", [5, 200, 1500])
+@pytest.mark.parametrize("width", [8, 64, 264, 1000, 4096, 32768])
+def test_rows_whose_squares_overflow(px, rows, width):
+    """Rows around the square root of fp32's largest number and up to bf16's own, between ordinary ones."""
+    x, r, g = _inputs(rows, width, seed=rows + width)
+    x[1::3] = (x[1::3].double() * 2.0**63).to(torch.bfloat16)
+    x[2, -1] = torch.finfo(torch.bfloat16).min
+    x[4] = torch.finfo(torch.bfloat16).max
+    r[4] = 0
+    out, res_out = torch.empty_like(x), torch.empty_like(x)
+    q, scale = torch.empty(x.shape, dtype=E4M3, device="cuda"), torch.empty(rows, device="cuda")
+    px.rms_norm(x, g, EPS, out=out, residual=r, residual_out=res_out, out_e4m3=q, out_scale=scale)
+    _check(x, r, g, out, res_out, q, scale)
+    if rows == 5:                                 # ordinary rows are the same bits alone
+        alone = torch.empty_like(x[3:4])
+        px.rms_norm(x[3:4], g, EPS, out=alone, residual=r[3:4])
+        assert torch.equal(alone, out[3:4])
 
 
 @pytest.mark.parametrize("size", [1e-18, 1e-30])
