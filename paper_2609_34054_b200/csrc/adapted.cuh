@@ -226,6 +226,18 @@ adapted_shrink_kernel(const AdaptedParams p) {
       clear();
     }
   }
+  // the scales of what this thread finishes below, on their way while the sums meet
+  constexpr int MINE = RT * R / SHRINK_THREADS > 0 ? RT * R / SHRINK_THREADS : 1;
+  float scale[MINE];
+#pragma unroll
+  for (int k = 0; k < MINE; ++k) {
+    const int i = threadIdx.x + ((int)rank_c + k * (int)KS) * SHRINK_THREADS, r = i / R, c = i % R;      // (R is 16 or more: at most two rows a warp)
+    scale[k] = p.s;
+    if constexpr (Q8) {
+      const int a = __shfl_sync(0xffffffffu, id, r & 31);
+      if (i < RT * R && a >= 0 && c < p.rank) scale[k] *= __ldg(p.a_scale + a * p.rank + c);
+    }
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < RT * R; i += SHRINK_THREADS) {
     const int r = i / R, c = i % R;
@@ -243,9 +255,10 @@ adapted_shrink_kernel(const AdaptedParams p) {
     __syncthreads();
   }
   // every block of the cluster finishes a share of the elements, adding the blocks' sums in rank order
-  for (int i = threadIdx.x + (int)rank_c * SHRINK_THREADS; i < RT * R; i += SHRINK_THREADS * (int)KS) {
-    const int r = i / R, c = i % R;
-    if (!((with_adapter >> r) & 1u)) continue;
+#pragma unroll
+  for (int j = 0; j < MINE; ++j) {
+    const int i = threadIdx.x + ((int)rank_c + j * (int)KS) * SHRINK_THREADS, r = i / R, c = i % R;
+    if (i >= RT * R || !((with_adapter >> r) & 1u)) continue;
     const uint32_t local = smem_u32(&part[r][c]);
     float u[8], v = 0.f;
 #pragma unroll
@@ -255,8 +268,7 @@ adapted_shrink_kernel(const AdaptedParams p) {
     }
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) v += u[k];
-    if constexpr (Q8) { if (c < p.rank) v *= p.a_scale[agent_of(p, row0 + r) * p.rank + c]; }
-    p.T[(row0 + r) * p.rank_pad + c] = __float2bfloat16(p.s * v);
+    p.T[(row0 + r) * p.rank_pad + c] = __float2bfloat16(scale[j] * v);
   }
   if (KS > 1) {
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");

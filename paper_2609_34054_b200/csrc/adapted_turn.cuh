@@ -272,15 +272,18 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     }
     if (n_units > 0) sync_merging();
     // ---- own rows + received rows, in rank order: sixteen threads per row, eight columns each
-    mbar_wait_cluster(recv_bar, 0, p.status);
     const float* own = dump + (size_t)rank * tw * PT_COLS;
     const int piece = et & 15, gc = n0 + piece * 8;
-    if (gc < p.N) {
-      float ws[8];
-      if constexpr (Q8) {
+    float ws[8], xs = 0.f;                               // 8 bits: the scales of this thread's columns and of its next row, ahead of the last wait
+    if constexpr (Q8) {
+      if (gc < p.N) {
         const float4 a = __ldg(reinterpret_cast<const float4*>(p.w_scale + gc)), b = __ldg(reinterpret_cast<const float4*>(p.w_scale + gc) + 1);
         ws[0] = a.x; ws[1] = a.y; ws[2] = a.z; ws[3] = a.w; ws[4] = b.x; ws[5] = b.y; ws[6] = b.z; ws[7] = b.w;
+        if ((et >> 4) < own_rows) xs = __ldg(p.x_scale + m0 + rank * tw + (et >> 4));
       }
+    }
+    mbar_wait_cluster(recv_bar, 0, p.status);
+    if (gc < p.N) {
       for (int r = et >> 4; r < own_rows; r += AT_EPI_WARPS * 2) {
         const long long m = m0 + rank * tw + r;
         float v[8];
@@ -299,9 +302,9 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
           }
         }
         if constexpr (Q8) {
-          const float xs = __ldg(p.x_scale + m);
 #pragma unroll
           for (int q = 0; q < 8; ++q) v[q] *= xs * ws[q];
+          if (r + AT_EPI_WARPS * 2 < own_rows) xs = __ldg(p.x_scale + m + AT_EPI_WARPS * 2);
         }
         *reinterpret_cast<uint4*>(p.y + m * p.N + gc) = pack_bf16x8(v);
       }

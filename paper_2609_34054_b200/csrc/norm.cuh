@@ -5,8 +5,8 @@
 // HBM-bound: a row is read once, kept in registers as fp32 from the addition to the last rounding (the norm is of the unrounded
 // sum; every output is rounded once), and written once.  A thread holds C pieces of eight columns, piece i of the row at thread
 // i % T, so that a warp's loads are 512 consecutive bytes.  32768 x 4096 with residual and 8-bit output: 136.7 us, 6.9 TB/s of
-// what is read and written, the rate of a plain copy; both outputs of 1337 x 3584 9.9 us (6.4 from L2).  One row: 1.6 us behind another kernel,
-// of which a kernel that does nothing takes most.
+// what is read and written, the rate of a plain copy; both outputs of 1337 x 3584 9.9 us (6.4 from L2).  One row: 1.65 us a call in a graph of
+// such calls.
 #pragma once
 #include "common.cuh"
 
