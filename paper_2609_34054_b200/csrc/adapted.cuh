@@ -5,6 +5,7 @@
 // dependent start as soon as all its own blocks run - behind its own wait for the kernel ahead, so whatever
 // the dependent reads before ITS wait was complete before either started - and uses little shared memory and few registers, so
 // that a block of the main kernel fits on the same SM.  For many rows it is a kernel on the tensor cores of its own (adapted_shrink.cuh).
+// For a decode step it is latency and no more (8 rows of 4096, eight agents of rank 32: 4.3 us beside a main kernel of 7), and so it is for 777 rows of 1024 (5.7).
 // T is rounded to bf16, the operand type of the MMA that takes it: 2^-8 of the adapter's term, which is added to a sum that is
 // rounded to bf16 as a whole.
 #pragma once

@@ -6,6 +6,9 @@
 // main loop runs), and a warp multiplies a group's rows of T with 64 columns of that agent's B by mma.sync: rows of different agents never share a
 // product.  B comes straight from global memory: a lane reads eight neighbouring columns of the four coordinates that the fragment wants
 // of it, and column 8 g + j belongs to column g of the j-th MMA, so that it holds sixteen neighbouring columns of the result.
+// Measured without / with adapters of rank 16, weights from HBM: 64 rows of 3584 x 3584 in bf16 8.8 / 14.0 us with the rows spread over eight agents, 12.7 with one (the
+// bytes alone take 4.4); 61 rows of 4096 x 4096 with 64 agents of rank 64, whose A and B are twice the weights, 10.2 / 32.  What bounds
+// it is latency: start, first copies, merge in the cluster, and ahead of it the start of the shrink kernel.
 // Where a block has few rows the products are taken while the main loop runs, into a place of their own; else a warp's first one is, in registers, and
 // all are added to the sums in shared memory.
 #pragma once
