@@ -131,6 +131,48 @@ def test_8_bits_match_the_definition(px, rows, k, n, rank):
     _run(px, rows, max(128, k // 128 * 128), n, rank, 5, "rows", True, seed=rank)
 
 
+def _far(px, rows, k, n, r, e4m3, tail_rows, tail_cols):
+    """A call whose last rows and columns lie past 2^31 elements; everything but those is zero.  Only the corner is compared."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows + k + n)
+    t = lambda *s, std=1.0: (torch.randn(s, device="cuda", generator=g) * std).to(torch.bfloat16)  # noqa: E731
+    x = torch.zeros((rows, k), dtype=torch.bfloat16, device="cuda")
+    x[-tail_rows:] = t(tail_rows, k)
+    w = torch.zeros((k, n), dtype=torch.bfloat16, device="cuda")
+    w[:, -tail_cols:] = t(k, tail_cols, std=0.02)
+    A, B = t(2, k, r, std=k ** -0.5), t(2, r, n, std=0.05)
+    wt = px.adapted_weights(w, A, B, 1.5, e4m3=e4m3)
+    ids = (torch.arange(rows, device="cuda") % 3 - 1).to(torch.int32)
+    out = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+    ws = px.adapted_workspace(wt, rows)
+    xt, wc = x[-tail_rows:], w[:, -tail_cols:].contiguous()
+    if e4m3:
+        xs = torch.ones(rows, device="cuda")
+        xq = torch.zeros((rows, k), dtype=E4M3, device="cuda")
+        xq[-tail_rows:] = xt.to(E4M3)
+        px.adapted_project_e4m3(wt, xq, xs, out, ids, ws)
+        wq, s = _quantised(wc)
+        xd, wd = xq[-tail_rows:].double(), wq.double() * s
+    else:
+        px.adapted_project(wt, x, out, ids, ws)
+        xd, wd = xt.double(), wc.double()
+    y, bound = _reference(xd, wd, A, B[:, :, -tail_cols:], ids[-tail_rows:], 1.5, e4m3)
+    assert ((out[-tail_rows:, -tail_cols:].double() - y).abs() <= bound).all()
+    assert (out[0, :-tail_cols] == 0).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows,k,n", [(270001, 128, 8192), (65601, 32768, 136)])
+def test_rows_past_32_bits(px, rows, k, n, e4m3):
+    _far(px, rows, k, n, 16, e4m3, 300, 64)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows", [4, 16, 100, 1000])
+def test_weights_past_32_bits(px, rows, e4m3):
+    _far(px, rows, 262144, 9472, 16, e4m3, min(rows, 50), 64)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("mix", ["none", "neutral", "one", "runs", "rows"])
 @pytest.mark.parametrize("rows", [1, 5, 31, 96, 300, 2200])
