@@ -7,9 +7,8 @@
 // another, so a block mostly sees one or two agents.  Where it sees more than 128 lanes hold, a step loads A for
 // several accumulators at once (CHUNKS), and beyond that the block goes over X again.
 // 8 bits: A is the sum of two e4m3 matrices (value and rest); both are added into the same accumulator.
-// Measured: 32768 x 4096 in bf16, runs of eight agents of rank 32, 49 us (5.5 TB/s of X); 8192 x 4096 22.7, where start and epilogue are a third, and 16.5
-// with one agent of rank 16.  Half as many tiles of twice the rows in clusters of two take 19 .. 21 there, but 70 instead of 49 for 32768 rows and 32 instead
-// of 23 for 16384 in 8 bits; k-blocks begun at another place in every block change nothing.
+// Measured: 32768 x 4096 in bf16, runs of eight agents of rank 32, 49 us (5.5 TB/s of X); 8192 x 4096 19.2, where start and epilogue are a third.
+// K-blocks begun at another place in every block change nothing.
 #pragma once
 #include "adapted.cuh"
 
