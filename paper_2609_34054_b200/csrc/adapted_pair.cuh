@@ -5,7 +5,7 @@
 // T rows as the A operand and that agent's B (columns contiguous in memory, so an MN-major operand) as the other.  The rows of a tile
 // are the lanes of the accumulator, and the MMA leaves the lanes of other agents' rows alone (its lane mask): no other adapter, were it
 // infinite or NaN, touches a row, and T needs no zeros for the rows of others.
-// Bound by the tensor pipe: 8192 rows of 4096 x 4096 in bf16 in 165 .. 172 us without adapters (1.6 .. 1.67 PFLOP/s, a large library product's rate; the pipe is active 83 %
+// Bound by the tensor pipe: 8192 rows of 4096 x 4096 in bf16 in 165 .. 172 us without adapters (1.6 .. 1.67 PFLOP/s, a large library product's rate; the pipe is active 81 .. 83 %
 // of the time), 99 us in 8 bits; with eight agents' runs of rank 32, the shrink kernel included, 197 .. 203.  In a long loop the power limit takes
 // clocks: 235.  512 rows are 17.5 us, as 64 tiles leave ten pairs of SMs idle and each loads at L2's rate.
 #pragma once
