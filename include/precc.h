@@ -444,6 +444,7 @@ int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, cons
  * 8 bits: X and W are e4m3, X[m] = x_scale[m] * X_e4m3[m] (as precc_rms_norm leaves it), W_packed and w_scale [n_out] from
  * precc_pack_kmajor_e4m3, A_packed and a_scale [n_agents*rank] from precc_pack_adapter_e4m3, B_packed from
  * precc_pack_expand_e4m3.
+ * Alignment in bytes: X, W_packed, A_packed, B, Y and w_scale 16; x_scale, a_scale and agent_id 4.
  * Supported: k_dim a multiple of 64 (8 bits: 128), n_out of 8, both up to 2^20; rank 0, 8, 16, 32 or 64; up to 64 agents;
  * M up to 2^26.  M == 0 is a no-op. */
 typedef struct {

@@ -191,8 +191,8 @@ adapted_shrink_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
             float4 v = *reinterpret_cast<const float4*>(dump + r * AS_DUMP_PITCH + at + k);
             float4 w = make_float4(p.s, p.s, p.s, p.s);
             if constexpr (Q8) {
-              const float4 sc = *reinterpret_cast<const float4*>(p.a_scale + (a << p.rank_shift) + k);
-              w = make_float4(p.s * sc.x, p.s * sc.y, p.s * sc.z, p.s * sc.w);
+              const float* sc = p.a_scale + (a << p.rank_shift) + k;        // (a caller's pointer, on a 4-byte boundary and no more)
+              w = make_float4(p.s * __ldg(sc), p.s * __ldg(sc + 1), p.s * __ldg(sc + 2), p.s * __ldg(sc + 3));
             }
             v = make_float4(v.x * w.x, v.y * w.y, v.z * w.z, v.w * w.w);
             if (KS > 1) {
