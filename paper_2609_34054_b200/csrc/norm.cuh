@@ -29,6 +29,22 @@ struct NormParams {
   float inv_width, eps;
 };
 
+// Sums, products and magnitudes that keep subnormal numbers, bf16's own among them (the library is built with flushing ones).
+__device__ __forceinline__ float add_full(float a, float b) {
+  float r;
+  asm("add.rn.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float mul_full(float a, float b) {
+  float r;
+  asm("mul.rn.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float abs_full(float a) {
+  float r;
+  asm("abs.f32 %0, %1;\n" : "=f"(r) : "f"(a));
+  return r;
+}
 // max that lets a NaN through (fmaxf drops it): a row with a NaN gets a NaN scale, not a plausible one
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -92,7 +108,7 @@ rms_norm_kernel(const NormParams p) {
     unpack_bf16x8(xv[c], s[c]);
     unpack_bf16x8(rv[c], r);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) { s[c][k] += r[k]; sum = fmaf(s[c][k], s[c][k], sum); }
+    for (int k = 0; k < 8; ++k) { s[c][k] = add_full(s[c][k], r[k]); sum = fmaf(s[c][k], s[c][k], sum); }
   }
   if (p.residual_out) {
 #pragma unroll
@@ -113,7 +129,7 @@ rms_norm_kernel(const NormParams p) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) { s[c][k] *= unit; sum = fmaf(s[c][k], s[c][k], sum); }
+      for (int k = 0; k < 8; ++k) { s[c][k] = mul_full(s[c][k], unit); sum = fmaf(s[c][k], s[c][k], sum); }
     sum = reduce(sum, 2, [](float a, float b) { return a + b; });
   }
   const float inv = 1.0f / sqrtf(fmaf(sum, p.inv_width, eps));
@@ -125,20 +141,22 @@ rms_norm_kernel(const NormParams p) {
       float g[8];
       unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(p.gain) + i), g);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) { s[c][k] = s[c][k] * inv * g[k]; top = max_nan(top, fabsf(s[c][k])); }
+      for (int k = 0; k < 8; ++k) { s[c][k] = mul_full(mul_full(s[c][k], inv), g[k]); top = max_nan(top, abs_full(s[c][k])); }
       if (p.out) reinterpret_cast<uint4*>(p.out)[at + i] = pack_bf16x8(s[c]);
     }
   }
   if (!p.q) return;
   top = reduce(top, 1, [](float a, float b) { return max_nan(a, b); });
-  const float scale = top == 0.f ? 1.f : max_nan(top * (1.f / E4M3_MAX), 1.17549435e-38f);     // (a normal number, and so is its reciprocal)
+  const float scale = __float_as_uint(top) == 0u ? 1.f : max_nan(top * (1.f / E4M3_MAX), 1.17549435e-38f);     // (a normal number, and so is its reciprocal)
   const float to_q = 1.0f / scale;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int i = t + c * p.T;
-    if (live && i < p.pieces)
-      reinterpret_cast<uint2*>(p.q)[at + i] = make_uint2(pack_e4m3x4(s[c][0] * to_q, s[c][1] * to_q, s[c][2] * to_q, s[c][3] * to_q),
-                                                         pack_e4m3x4(s[c][4] * to_q, s[c][5] * to_q, s[c][6] * to_q, s[c][7] * to_q));
+    if (live && i < p.pieces) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[c][k] = mul_full(s[c][k], to_q);
+      reinterpret_cast<uint2*>(p.q)[at + i] = make_uint2(pack_e4m3x4(s[c][0], s[c][1], s[c][2], s[c][3]), pack_e4m3x4(s[c][4], s[c][5], s[c][6], s[c][7]));
+    }
   }
   if (live && t == 0) p.q_scale[row] = scale;
 }
