@@ -37,7 +37,7 @@ int32_t norm_launch(precc_ctx* ctx, const NormParams& p, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  PRECC_CUDA(ctx, cudaLaunchKernelEx(&cfg, rms_norm_kernel<C, SHORT>, p));
+  PRECC_CUDA(ctx, p.residual ? cudaLaunchKernelEx(&cfg, rms_norm_kernel<C, SHORT, true>, p) : cudaLaunchKernelEx(&cfg, rms_norm_kernel<C, SHORT, false>, p));
   return PRECC_OK;
 }
 

@@ -18,7 +18,7 @@ constexpr float E4M3_MAX = 448.f;
 
 struct NormParams {
   const __nv_bfloat16* x;
-  const __nv_bfloat16* residual;             // or null
+  const __nv_bfloat16* residual;             // RES
   const __nv_bfloat16* gain;
   __nv_bfloat16* residual_out;               // or null
   __nv_bfloat16* out;                        // or null
@@ -67,8 +67,8 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&f)[8]) {
 }
 
 // C pieces per thread.  SHORT: several rows of T <= 32 threads (a power of two) in a block of NORM_SHORT_THREADS; else one row
-// of blockDim.x = T threads.
-template <int C, bool SHORT>
+// of blockDim.x = T threads.  RES: with a residual.
+template <int C, bool SHORT, bool RES>
 __global__ void __launch_bounds__(SHORT ? NORM_SHORT_THREADS : 1024)
 rms_norm_kernel(const NormParams p) {
   __shared__ float part[3][32];
@@ -90,6 +90,8 @@ rms_norm_kernel(const NormParams p) {
   pdl_wait();
   pdl_launch_dependents();
   const long long at = row * p.pieces;       // in pieces of eight columns
+  // s[c][k]: x, or with a residual half of the sum, as the whole one may pass fp32's largest number (a power of two changes no rounding, and bf16's
+  // least subnormal has a half in fp32).  The norm is the same with eps in these units, a quarter of it.
   float s[C][8];
   float sum = 0.f;
   uint4 xv[C], rv[C];
@@ -99,7 +101,7 @@ rms_norm_kernel(const NormParams p) {
     xv[c] = rv[c] = make_uint4(0, 0, 0, 0);
     if (live && i < p.pieces) {
       xv[c] = reinterpret_cast<const uint4*>(p.x)[at + i];
-      if (p.residual) rv[c] = reinterpret_cast<const uint4*>(p.residual)[at + i];
+      if (RES) rv[c] = reinterpret_cast<const uint4*>(p.residual)[at + i];
     }
   }
 #pragma unroll
@@ -108,19 +110,27 @@ rms_norm_kernel(const NormParams p) {
     unpack_bf16x8(xv[c], s[c]);
     unpack_bf16x8(rv[c], r);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) { s[c][k] = add_full(s[c][k], r[k]); sum = fmaf(s[c][k], s[c][k], sum); }
+    for (int k = 0; k < 8; ++k) {
+      s[c][k] = RES ? add_full(mul_full(s[c][k], 0.5f), mul_full(r[k], 0.5f)) : add_full(s[c][k], 0.f);       // (-0 is 0)
+      sum = fmaf(s[c][k], s[c][k], sum);
+    }
   }
   if (p.residual_out) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int i = t + c * p.T;
-      if (live && i < p.pieces) reinterpret_cast<uint4*>(p.residual_out)[at + i] = pack_bf16x8(s[c]);
+      if (live && i < p.pieces) {
+        float whole[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) whole[k] = RES ? add_full(s[c][k], s[c][k]) : s[c][k];
+        reinterpret_cast<uint4*>(p.residual_out)[at + i] = pack_bf16x8(whole);
+      }
     }
   }
   sum = reduce(sum, 0, [](float a, float b) { return a + b; });
-  float eps = p.eps;
+  float eps = RES ? 0.25f * p.eps : p.eps;
   // Squares past fp32's range (values above 2^56, such as a type's lowest one): the row, and eps with it, in units of 2^72, which leaves 32768 squares of the
-  // largest sums in range.  y is the same.  (Rows that share a warp go through it together, each with its own unit.)
+  // largest values in range.  y is the same.  (Rows that share a warp go through it together, each with its own unit.)
   const bool over = isinf(sum);
   if (SHORT ? __any_sync(0xffffffffu, over) : over) {
     const float unit = over ? 0x1p-72f : 1.f;

@@ -1,4 +1,4 @@
-"""precc_rms_norm at the ends of bf16's range: subnormal values among ordinary ones."""
+"""precc_rms_norm at the ends of bf16's range: sums past fp32's largest number, subnormal values among ordinary ones."""
 import pytest
 import torch
 
@@ -44,6 +44,20 @@ def _gain(width):
 
 
 SHAPES = [(1, 8), (5, 64), (300, 264), (1500, 128), (1300, 1000), (200, 4096), (3, 32768)]
+
+
+@pytest.mark.parametrize("rows,width", SHAPES)
+def test_sums_past_fp32(px, rows, width):  # noqa: F811
+    """x + residual passes fp32's largest number where both are near bf16's."""
+    x, r = _rows(rows, width, 1.0, seed=width)
+    x[0] = r[0] = TOP
+    m = rows // 2
+    x[m, ::2] = r[m, ::2] = -TOP
+    x[m, 1::4], r[m, 1::4] = TOP, -TOP
+    if rows > 1:                                 # (a row of its own: the one above times 2^125 would hold infinities)
+        x[rows - 1] = (x[rows - 1].double() * 2.0**125).to(BF16)
+        r[rows - 1, -1] = TOP
+    _check(px, x, r, _gain(width), 1e-5)
 
 
 @pytest.mark.parametrize("rows,width", SHAPES)
