@@ -128,21 +128,23 @@ rms_norm_kernel(const NormParams p) {
     }
   }
   sum = reduce(sum, 0, [](float a, float b) { return a + b; });
-  float eps = RES ? 0.25f * p.eps : p.eps;
+  float mean = fmaf(sum, p.inv_width, RES ? 0.25f * p.eps : p.eps);
   // Squares past fp32's range (values above 2^56, such as a type's lowest one): the row, and eps with it, in units of 2^72, which leaves 32768 squares of the
-  // largest values in range.  y is the same.  (Rows that share a warp go through it together, each with its own unit.)
-  const bool over = isinf(sum);
-  if (SHORT ? __any_sync(0xffffffffu, over) : over) {
-    const float unit = over ? 0x1p-72f : 1.f;
-    eps *= unit * unit;
+  // largest values in range.  Squares that vanish (below 2^-126, so at most 2^-126 of the mean) where neither the others nor eps outweigh
+  // them: in units of 2^-100, where the least subnormal's does not vanish and a mean of 2^-100 is in range.  y is the same.  (Rows that share a
+  // warp go through it together, each with its own unit.)
+  const bool over = isinf(sum), under = mean < 0x1p-100f;
+  if (SHORT ? __any_sync(0xffffffffu, over || under) : over || under) {
+    const float unit = over ? 0x1p-72f : under ? 0x1p100f : 1.f;
     sum = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < 8; ++k) { s[c][k] = mul_full(s[c][k], unit); sum = fmaf(s[c][k], s[c][k], sum); }
     sum = reduce(sum, 2, [](float a, float b) { return a + b; });
+    mean = fmaf(sum, p.inv_width, mul_full(mul_full(p.eps, unit), RES ? 0.25f * unit : unit));
   }
-  const float inv = 1.0f / sqrtf(fmaf(sum, p.inv_width, eps));
+  const float inv = 1.0f / sqrtf(mean);
   float top = 0.f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {

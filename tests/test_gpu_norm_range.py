@@ -1,4 +1,5 @@
-"""precc_rms_norm at the ends of bf16's range: sums past fp32's largest number, subnormal values among ordinary ones."""
+"""precc_rms_norm at the ends of bf16's range: no eps or a tiny one under rows whose squares vanish, sums past fp32's largest number, subnormal
+values among ordinary ones."""
 import pytest
 import torch
 
@@ -44,6 +45,25 @@ def _gain(width):
 
 
 SHAPES = [(1, 8), (5, 64), (300, 264), (1500, 128), (1300, 1000), (200, 4096), (3, 32768)]
+
+
+@pytest.mark.parametrize("size", [1e-17, 1e-19, 1e-21, 1e-25, 1e-32, 1e-37, 1e-39])
+@pytest.mark.parametrize("rows,width", SHAPES)
+def test_tiny_rows_without_eps(px, rows, width, size):  # noqa: F811
+    x, r = _rows(rows, width, size, seed=width)
+    x[:, 0] = size                               # (no row of zeros: without eps that is 0 / 0)
+    r[:, 0] = 0
+    x[rows // 2] = (I.normal_bf16((width,), 1.0, 1, "range.mid").cuda())
+    r[rows // 2] = 0
+    _check(px, x, r, _gain(width), 0.0)
+
+
+@pytest.mark.parametrize("eps", [1e-45, 1e-41, 1e-38, 1e-34, 1e-30, 1e-24])
+@pytest.mark.parametrize("size", [1e-12, 1e-17, 1e-19, 1e-22, 1e-30, 1e-39])
+def test_tiny_rows_with_a_tiny_eps(px, eps, size):  # noqa: F811
+    x, r = _rows(37, 520, size, seed=4)
+    x[3], r[3] = 0, 0
+    _check(px, x, r, _gain(520), eps)
 
 
 @pytest.mark.parametrize("rows,width", SHAPES)
