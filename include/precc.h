@@ -420,7 +420,8 @@ int32_t precc_combine_partials(precc_ctx* ctx, const precc_layer_desc* desc, con
  *   gain          [width]
  *   out_e4m3      [rows][width] e4m3 and out_scale, device fp32 [rows], go together; both NULL: no 8-bit output.  The
  *                 scale of a row of zeros is 1; scales are not smaller than the least normal fp32.
- * Outputs may be x or residual themselves (the same address); other overlaps are not allowed.  A row with a NaN or an infinity is NaN
+ * residual_out and out may be x or residual themselves (the same address).  Other overlaps of an output with an input or with another
+ * output are refused, the 8-bit output's among them: its rows would lie on other rows of x.  A row with a NaN or an infinity is NaN
  * in that place of `out` or in all of it, has a NaN or infinite scale, and touches no other row.  The norm is of
  * the unrounded sum, over the whole range of bf16.  width: a multiple of 8, at most 32768.  rows == 0 is a no-op. */
 int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, const void* gain, int32_t rows,

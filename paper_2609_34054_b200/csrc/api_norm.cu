@@ -26,6 +26,16 @@ NormPlan plan_norm(int rows, int pieces, bool residual) {
   return {c, whole_warps(c), false};
 }
 
+// Two buffers of a call that share bytes.
+struct Buffer { const void* p; size_t bytes; };
+bool overlap(const Buffer& a, const Buffer& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+// A thread reads its pieces of x and residual before it writes the same pieces of bf16, so those outputs may be x or residual as a whole.  Bytes of 8 bits lie
+// on other rows' values, which their blocks may not have read, and two outputs on one place have no order.
+bool overlap_allowed(const Buffer& out, const Buffer& in) { return !overlap(out, in) || (out.p == in.p && out.bytes == in.bytes); }
+
 template <int C, bool SHORT>
 int32_t norm_launch(precc_ctx* ctx, const NormParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
@@ -57,6 +67,14 @@ extern "C" int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* res
   if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(residual_out) || !aligned16(out) || !aligned16(out_e4m3) ||
       (reinterpret_cast<uintptr_t>(out_scale) & 3u))
     return fail(ctx, PRECC_ERR_MISALIGNED, "x / residual / gain / residual_out / out / out_e4m3 not 16-byte aligned (out_scale: 4)");
+  const size_t n = (size_t)rows * width;
+  const Buffer bx{x, 2 * n}, br{residual, 2 * n}, bg{gain, 2 * (size_t)width}, outs[4] = {{residual_out, 2 * n}, {out, 2 * n}, {out_e4m3, n}, {out_scale, 4 * (size_t)rows}};
+  for (int i = 0; i < 4; ++i) {
+    bool fine = !overlap(outs[i], bg);
+    for (const Buffer& in : {bx, br}) fine = fine && (i < 2 ? overlap_allowed(outs[i], in) : !overlap(outs[i], in));
+    for (int j = 0; j < i; ++j) fine = fine && !overlap(outs[i], outs[j]);
+    if (!fine) return fail(ctx, PRECC_ERR_INVALID_ARG, "outputs overlap an input or one another (only residual_out and out may be x or residual themselves)");
+  }
   const int32_t rc = check_device(ctx);
   if (rc) return rc;
   NormParams p;
