@@ -54,6 +54,10 @@ struct RingWalk {
   }
 };
 
+// 8 bits: a sum in units of its column's and its row's scale.  One scale after the other, and subnormal numbers kept: the product of the two may leave
+// fp32's range where the result does not (the norm leaves row scales down to 2^-126).
+__device__ __forceinline__ float unscale(float v, float w_scale, float x_scale) { return mul_full(mul_full(v, w_scale), x_scale); }
+
 // An agent id as the kernels use it: out of range counts as "no adapter" (reported by the shrink kernel).
 __device__ __forceinline__ int agent_of(const AdaptedParams& p, long long row) {
   if (row >= p.M) return -1;

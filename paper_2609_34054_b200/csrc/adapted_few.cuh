@@ -121,13 +121,14 @@ adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) red[warp][n * 8 + 2 * t + (e & 1)][g + 8 * (e >> 1)] = acc[n][e];
 
-  constexpr int MINE = 8 * NT * C / AF_THREADS > 0 ? 8 * NT * C / AF_THREADS : 1;       // what this thread finishes, and its scale
-  float scale[MINE];
+  constexpr int MINE = 8 * NT * C / AF_THREADS > 0 ? 8 * NT * C / AF_THREADS : 1;       // what this thread finishes (in one column), and its scales
+  float xs[MINE], ws = 1.f;
+  if constexpr (Q8) { if (n0 + (int)threadIdx.x % C < p.N) ws = __ldg(p.w_scale + n0 + threadIdx.x % C); }
 #pragma unroll
   for (int j = 0; j < MINE; ++j) {
-    const int i = threadIdx.x + j * AF_THREADS, r = i / C, c = i % C;
-    scale[j] = 1.f;
-    if constexpr (Q8) { if (r < p.M && n0 + c < p.N) scale[j] = __ldg(p.x_scale + r) * __ldg(p.w_scale + n0 + c); }
+    const int r = (threadIdx.x + j * AF_THREADS) / C;
+    xs[j] = 1.f;
+    if constexpr (Q8) { if (r < p.M) xs[j] = __ldg(p.x_scale + r); }
   }
   if (adapters) {
     pdl_wait();                                   // T is complete
@@ -175,7 +176,7 @@ adapted_few_kernel(const AdaptedParams p, const uint8_t* __restrict__ W) {
     float v = (with_adapter >> r) & 1u ? low[r][c] : 0.f;
 #pragma unroll
     for (int w = 0; w < AF_WARPS; ++w) v += red[w][r][c];
-    p.y[(long long)r * p.N + n0 + c] = __float2bfloat16(v * scale[j]);
+    p.y[(long long)r * p.N + n0 + c] = __float2bfloat16(Q8 ? unscale(v, ws, xs[j]) : v);
   }
 }
 

@@ -203,8 +203,8 @@ adapted_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
           for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[8 * q + k]);
           if constexpr (Q8) {
             const float4 u = *reinterpret_cast<const float4*>(&w_scale_s[buf][c + 8 * q]), w = *reinterpret_cast<const float4*>(&w_scale_s[buf][c + 8 * q + 4]);
-            v[0] *= xs * u.x; v[1] *= xs * u.y; v[2] *= xs * u.z; v[3] *= xs * u.w;
-            v[4] *= xs * w.x; v[5] *= xs * w.y; v[6] *= xs * w.z; v[7] *= xs * w.w;
+            v[0] = unscale(v[0], u.x, xs); v[1] = unscale(v[1], u.y, xs); v[2] = unscale(v[2], u.z, xs); v[3] = unscale(v[3], u.w, xs);
+            v[4] = unscale(v[4], w.x, xs); v[5] = unscale(v[5], w.y, xs); v[6] = unscale(v[6], w.z, xs); v[7] = unscale(v[7], w.w, xs);
           }
           if (n0 + c + 8 * q < p.N) *reinterpret_cast<uint4*>(yr + c + 8 * q) = pack_bf16x8(v);       // (N is a multiple of 8)
         }

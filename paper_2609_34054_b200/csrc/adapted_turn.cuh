@@ -306,7 +306,7 @@ adapted_turn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         }
         if constexpr (Q8) {
 #pragma unroll
-          for (int q = 0; q < 8; ++q) v[q] *= xs * ws[q];
+          for (int q = 0; q < 8; ++q) v[q] = unscale(v[q], ws[q], xs);
           if (r + AT_EPI_WARPS * 2 < own_rows) xs = __ldg(p.x_scale + m + AT_EPI_WARPS * 2);
         }
         *reinterpret_cast<uint4*>(p.y + m * p.N + gc) = pack_bf16x8(v);
