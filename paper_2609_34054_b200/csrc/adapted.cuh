@@ -273,7 +273,8 @@ adapted_shrink_kernel(const AdaptedParams p) {
     }
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) v += u[k];
-    p.T[(row0 + r) * p.rank_pad + c] = __float2bfloat16(scale[j] * v);
+    // (rank 8: the other eight of an MMA's sixteen coordinates are zeros, in a row with an infinity too, where the product gave 0 * inf)
+    p.T[(row0 + r) * p.rank_pad + c] = __float2bfloat16(c < p.rank ? scale[j] * v : 0.f);
   }
   if (KS > 1) {
     asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");

@@ -1,4 +1,4 @@
-"""The adapted projections at the ends of the range: row and column scales of 8 bits whose product leaves fp32's."""
+"""The adapted projections at the ends of the range: row and column scales of 8 bits whose product leaves fp32's, rows with infinities."""
 import pytest
 import torch
 
@@ -54,3 +54,29 @@ def test_zeros_under_scales_whose_product_overflows(px, rows, row_scale, w_std):
     out = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
     px.adapted_project_e4m3(wt, xq, torch.full((rows,), row_scale, device="cuda"), out)
     assert (out == 0).all()
+
+
+def _infinite_row(px, rows, rank):
+    """Weights and adapters above zero: a row with an infinity is infinite in every column, and no padding of the rank makes it NaN."""
+    k, n, agents = 256, 72, 3
+    x, w, A, B = (t.abs() + 0.01 for t in _draw(k, n, rank, agents, rows))
+    ids = _ids(rows, agents, "one")
+    ws = px.adapted_workspace(px.adapted_weights(w, A, B, 1.0), rows).fill_(255)
+    x[rows // 2, 3] = float("inf")
+    out = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+    px.adapted_project(px.adapted_weights(w, A, B, 1.0), x, out, ids, ws)
+    assert (out[rows // 2] == float("inf")).all()
+    others = torch.arange(rows, device="cuda") != rows // 2
+    assert torch.isfinite(out[others]).all()
+
+
+@pytest.mark.parametrize("rank", [8, 16, 64])
+@pytest.mark.parametrize("rows", [1, 9, 30, 70, 700, 2500])
+def test_a_row_with_an_infinity(px, rows, rank):  # noqa: F811
+    _infinite_row(px, rows, rank)
+
+
+@pytest.mark.parametrize("rank", [8, 32])
+@pytest.mark.parametrize("rows", [5, 70, 300])
+def test_a_row_with_an_infinity_in_every_kernel(forced, rows, rank):  # noqa: F811
+    _infinite_row(forced, rows, rank)
