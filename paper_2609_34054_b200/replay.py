@@ -222,6 +222,7 @@ def _replay_db(st: Stack, turns: Sequence[Turn]) -> Dict[str, float]:
         masks_2n = torch.tensor([1 << j] * n + [others] * n, dtype=torch.int64, device=dev)
         # agent j's own LR rows also go to the tokens' shared slots: they outlive the private blocks
         copy_2n = torch.cat([P + torch.arange(n, dtype=torch.int32), torch.full((n,), -1, dtype=torch.int32)]).to(dev)
+        agents_2n = torch.tensor([j] * n + [-1] * n, dtype=torch.int32, device=dev)
 
         st.H2[:n].copy_(st.H_adpt[P:P + n])                           # the two sequences of the turn, one batch
         st.H2[n:2 * n].copy_(st.H_neut[P:P + n])
@@ -243,7 +244,7 @@ def _replay_db(st: Stack, turns: Sequence[Turn]) -> Dict[str, float]:
                 px.lr_attend_prefill(st.desc, q[:n], j, P, st.B_k[k], st.B_v[k], st.caches[l], out[:n], table_a)
                 px.lr_attend_prefill(st.desc, q[-n:], -1, P, st.B_k[k], st.B_v[k], st.caches[l], out[-n:])
             if st.blocks:
-                st.blocks.forward(st.H2[:2 * n], torch.tensor([j] * n + [-1] * n, dtype=torch.int32, device=dev), layer)
+                st.blocks.forward(st.H2[:2 * n], agents_2n, layer)
             else:
                 for l in range(st.n_layers):
                     layer(l, st.H2[:2 * n], st.q[:n], st.out[:n])
