@@ -408,6 +408,11 @@ class Precc:
         agents, r = (A.shape[0], A.shape[2]) if A is not None and A.dim() == 3 else (0, 0)
         if A is not None and (A.shape != (agents, k, r) or B.shape != (agents, r, n) or A.dtype != W.dtype or B.dtype != W.dtype):
             raise PreccError("A must be bf16 [agents, k, r] and B bf16 [agents, r, n]")
+        # (the packing kernels run on the current device, and an address of another one is none there)
+        if any(t is not None and (t.get_device() != self.device or not t.is_contiguous()) for t in (W, A, B)):
+            raise PreccError(f"W, A and B must be contiguous tensors on the context's device {self.device}")
+        if torch.cuda.current_device() != self.device:
+            raise PreccError(f"the context's device {self.device} is not the current one")
         w_scale = None
         if e4m3:
             packed = torch.empty((k // 128, n, 128), dtype=torch.float8_e4m3fn, device=W.device)
