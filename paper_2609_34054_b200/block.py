@@ -27,6 +27,8 @@ class AttentionBlocks:
     """Weights, residual stream and scratch of a stack of layers (distinct weights per layer unless ``shared_weights``)."""
 
     def __init__(self, px: Precc, geo: I.Geometry, n_layers: int, max_rows: int, seed: int = 0, shared_weights: bool = False, e4m3: bool = False):
+        if n_layers < 1 or max_rows < 1:
+            raise ValueError("a stack of blocks has at least one layer and one row")
         self.px, self.geo, self.n_layers, self.e4m3 = px, geo, n_layers, e4m3
         d, width = geo.d_model, geo.n_q * geo.hd
         scale = geo.scale(geo.rank_v)
@@ -50,6 +52,8 @@ class AttentionBlocks:
         layer's caches and the attention of q [n, n_q, hd] into out.  Returns the residual stream after the last layer (a buffer
         of this object, overwritten by the next call)."""
         n, px, geo = x.shape[0], self.px, self.geo
+        if n > self.r.shape[0] or x.shape[1:] != self.r.shape[1:]:
+            raise ValueError(f"x is {tuple(x.shape)}, the blocks take up to {self.r.shape[0]} rows of {self.r.shape[1]}")
         r, h, y, q, o = (t[:n] for t in (self.r, self.h, self.y, self.q, self.o))
         h8, hs = (self.h8[:n], self.h_scale[:n]) if self.e4m3 else (None, None)
         r.copy_(x)
