@@ -26,15 +26,26 @@ NormPlan plan_norm(int rows, int pieces, bool residual) {
   return {c, whole_warps(c), false};
 }
 
-// Two buffers of a call that share bytes.
-struct Buffer { const void* p; size_t bytes; };
-bool overlap(const Buffer& a, const Buffer& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+// Whether a_bytes from a on and b_bytes from b on share any.
+inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return b && x < y + b_bytes && y < x + a_bytes;
 }
 // A thread reads its pieces of x and residual before it writes the same pieces of bf16, so those outputs may be x or residual as a whole.  Bytes of 8 bits lie
-// on other rows' values, which their blocks may not have read, and two outputs on one place have no order.
-bool overlap_allowed(const Buffer& out, const Buffer& in) { return !overlap(out, in) || (out.p == in.p && out.bytes == in.bytes); }
+// on other rows' values, which their blocks may not have read, and two outputs on one place have no order.  (A decode step's call has two outputs: what
+// is not given costs nothing here.)
+bool outputs_apart(const void* x, const void* residual, const void* gain, size_t rows, size_t width, const void* residual_out, const void* out, const void* q,
+                   const void* scale) {
+  const size_t n = rows * width;
+  auto meets_input = [&](const void* o, size_t bytes, bool may_be) {
+    return (overlap(o, bytes, x, 2 * n) && !(may_be && o == x)) || (overlap(o, bytes, residual, 2 * n) && !(may_be && o == residual)) || overlap(o, bytes, gain, 2 * width);
+  };
+  if (residual_out && meets_input(residual_out, 2 * n, true)) return false;
+  if (out && (meets_input(out, 2 * n, true) || overlap(out, 2 * n, residual_out, 2 * n))) return false;
+  if (!q) return true;
+  return !meets_input(q, n, false) && !meets_input(scale, 4 * rows, false) && !overlap(q, n, residual_out, 2 * n) && !overlap(q, n, out, 2 * n) && !overlap(q, n, scale, 4 * rows) &&
+         !overlap(scale, 4 * rows, residual_out, 2 * n) && !overlap(scale, 4 * rows, out, 2 * n);
+}
 
 template <int C, bool SHORT>
 int32_t norm_launch(precc_ctx* ctx, const NormParams& p, cudaStream_t stream) {
@@ -67,14 +78,8 @@ extern "C" int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* res
   if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(residual_out) || !aligned16(out) || !aligned16(out_e4m3) ||
       (reinterpret_cast<uintptr_t>(out_scale) & 3u))
     return fail(ctx, PRECC_ERR_MISALIGNED, "x / residual / gain / residual_out / out / out_e4m3 not 16-byte aligned (out_scale: 4)");
-  const size_t n = (size_t)rows * width;
-  const Buffer bx{x, 2 * n}, br{residual, 2 * n}, bg{gain, 2 * (size_t)width}, outs[4] = {{residual_out, 2 * n}, {out, 2 * n}, {out_e4m3, n}, {out_scale, 4 * (size_t)rows}};
-  for (int i = 0; i < 4; ++i) {
-    bool fine = !overlap(outs[i], bg);
-    for (const Buffer& in : {bx, br}) fine = fine && (i < 2 ? overlap_allowed(outs[i], in) : !overlap(outs[i], in));
-    for (int j = 0; j < i; ++j) fine = fine && !overlap(outs[i], outs[j]);
-    if (!fine) return fail(ctx, PRECC_ERR_INVALID_ARG, "outputs overlap an input or one another (only residual_out and out may be x or residual themselves)");
-  }
+  if (!outputs_apart(x, residual, gain, rows, width, residual_out, out, out_e4m3, out_scale))
+    return fail(ctx, PRECC_ERR_INVALID_ARG, "outputs overlap an input or one another (only residual_out and out may be x or residual themselves)");
   const int32_t rc = check_device(ctx);
   if (rc) return rc;
   NormParams p;

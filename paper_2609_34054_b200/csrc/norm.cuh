@@ -40,6 +40,11 @@ __device__ __forceinline__ float mul_full(float a, float b) {
   asm("mul.rn.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+__device__ __forceinline__ float fma_full(float a, float b, float c) {
+  float r;
+  asm("fma.rn.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ float abs_full(float a) {
   float r;
   asm("abs.f32 %0, %1;\n" : "=f"(r) : "f"(a));
@@ -111,7 +116,7 @@ rms_norm_kernel(const NormParams p) {
     unpack_bf16x8(rv[c], r);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      s[c][k] = RES ? add_full(mul_full(s[c][k], 0.5f), mul_full(r[k], 0.5f)) : add_full(s[c][k], 0.f);       // (-0 is 0)
+      s[c][k] = RES ? fma_full(s[c][k], 0.5f, mul_full(r[k], 0.5f)) : add_full(s[c][k], 0.f);       // (-0 is 0)
       sum = fmaf(s[c][k], s[c][k], sum);
     }
   }
