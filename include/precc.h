@@ -415,6 +415,7 @@ int32_t precc_combine_partials(precc_ctx* ctx, const precc_layer_desc* desc, con
 /* Root-mean-square norm with the residual's addition, row by row, in fp32:
  *   s = x + residual,  residual_out = bf16(s),  y = s / sqrt(mean(s^2) + eps) * gain
  *   out = bf16(y);  out_scale = max |y| / 448 of the row, out_e4m3 = e4m3(y / out_scale)
+ *   (quotients by a product with fp32's reciprocal: within 2^-21 of their size)
  *   x, residual, residual_out, out  [rows][width]; residual NULL: s = x; residual_out NULL: not written; out may be NULL when
  *                 out_e4m3 is given
  *   gain          [width]
@@ -423,7 +424,8 @@ int32_t precc_combine_partials(precc_ctx* ctx, const precc_layer_desc* desc, con
  * residual_out and out may be x or residual themselves (the same address).  Other overlaps of an output with an input or with another
  * output are refused, the 8-bit output's among them: its rows would lie on other rows of x.  A row with a NaN or an infinity is NaN
  * in that place of `out` or in all of it, has a NaN or infinite scale, and touches no other row.  The norm is of
- * the unrounded sum, over the whole range of bf16.  width: a multiple of 8, at most 32768.  rows == 0 is a no-op. */
+ * the unrounded sum, over the whole range of bf16 (subnormals, sums past bf16's largest number, and any eps from 0 on; a row
+ * of zeros with eps 0 is NaN, and a y past fp32's range infinite).  width: a multiple of 8, at most 32768.  rows == 0 is a no-op. */
 int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, const void* gain, int32_t rows,
                        int32_t width, float eps, void* residual_out, void* out, void* out_e4m3,
                        float* out_scale, void* stream);
@@ -444,7 +446,7 @@ int32_t precc_rms_norm(precc_ctx* ctx, const void* x, const void* residual, cons
  * on M, the sizes and the device, not on the other rows' agents.
  * 8 bits: X and W are e4m3, X[m] = x_scale[m] * X_e4m3[m] (as precc_rms_norm leaves it), W_packed and w_scale [n_out] from
  * precc_pack_kmajor_e4m3, A_packed and a_scale [n_agents*rank] from precc_pack_adapter_e4m3, B_packed from
- * precc_pack_expand_e4m3.
+ * precc_pack_expand_e4m3.  A sum is multiplied by w_scale, then by x_scale: their product may leave fp32's range.
  * Alignment in bytes: X, W_packed, A_packed, B, Y and w_scale 16; x_scale, a_scale and agent_id 4.
  * Supported: k_dim a multiple of 64 (8 bits: 128), n_out of 8, both up to 2^20; rank 0, 8, 16, 32 or 64; up to 64 agents;
  * M up to 2^26.  M == 0 is a no-op. */
@@ -474,7 +476,8 @@ int32_t precc_pack_kmajor_e4m3(precc_ctx* ctx, const void* src, int32_t k_dim, i
  * |A| is at least 2^-9 of the coordinate's largest, off by at most 2^-17 of that below.  A must be finite. */
 int32_t precc_pack_adapter_e4m3(precc_ctx* ctx, const void* A, int32_t k_dim, int32_t rank, int32_t agent,
                                 int32_t n_agents, void* dst, float* scale, void* stream);
-/* B bf16 [rows][n_cols] -> dst = bf16(B / w_scale[column]) (exact for powers of two). */
+/* B bf16 [rows][n_cols] -> dst = bf16(B / w_scale[column]): exact where w_scale is a power of two and the quotient a normal bf16 number
+ * (smaller quotients become 0, larger ones infinite). */
 int32_t precc_pack_expand_e4m3(precc_ctx* ctx, const void* B, int32_t rows, int32_t n_cols, const float* w_scale,
                                void* dst, void* stream);
 

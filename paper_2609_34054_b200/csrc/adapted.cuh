@@ -3,8 +3,9 @@
 //
 // T is small work (2 M K r flops) that the main kernel needs only at its end.  For few rows it runs beside it: the shrink kernel lets its
 // dependent start as soon as all its own blocks run - behind its own wait for the kernel ahead, so whatever
-// the dependent reads before ITS wait was complete before either started - and uses little shared memory and few registers, so
-// that a block of the main kernel fits on the same SM.  For many rows it is a kernel on the tensor cores of its own (adapted_shrink.cuh).
+// the dependent reads before ITS wait was complete before either started - and uses little shared memory and at most half of an SM's registers (90 .. 128 a
+// thread; the forms of 16 or 32 rows, and most in 8 bits, spill 4 .. 116 bytes at that limit), so that a block of the main kernel fits on the same SM (not
+// one of the few-row kernel for 17 .. 32 rows, with 178 registers, in 8 bits 255 and 108 bytes of spills).  For many rows it is a kernel on the tensor cores of its own (adapted_shrink.cuh).
 // For a decode step it is latency and no more (8 rows of 4096, eight agents of rank 32: 4.3 us beside a main kernel of 7), and so it is for 777 rows of 1024 (5.7).
 // T is rounded to bf16, the operand type of the MMA that takes it: 2^-8 of the adapter's term, which is added to a sum that is
 // rounded to bf16 as a whole.

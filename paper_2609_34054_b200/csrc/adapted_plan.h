@@ -12,10 +12,13 @@ constexpr int AP_MAX_AGENTS = 64;
 constexpr int AP_ROW_BYTES = 128;             // bytes of K in a k-block: 64 bf16 or 128 e4m3
 
 // ---- few rows (adapted_few.cuh): up to sixteen with at most two waves of blocks of sixteen columns (two blocks an SM), up to 32, where a block holds an SM, with one;
-// past eight rows, where every step costs a warp more, none that its eight warps need more than eight steps for.  us, few / turn kernel, rank 16, bf16:
+// past eight rows, where every step costs a warp more, none deeper than 4096 (eight steps of its eight warps in bf16, four in 8 bits).  us, few / turn kernel, rank 16, bf16:
 // 8 rows, 4096 x 4096 10.7 / 13.9, 4096 x 9472 17.6 / 18.9, 8192 x 1024 9.1 / 11.0, but 4096 x 14336 24.5 / 22.3; 16 rows, 4096 x 4096 11.7 / 13.1,
 // 4096 x 9472 19.0 / 19.9, 2048 x 2048 6.5 / 9.0, but 7168 x 2048 14.8 / 12.7; 32 rows, 2048 x 2048 8.7 / 10.3, 3584 x 1280 10.9 / 11.4, but 4096 x 4096
-// 17.8 / 13.3 and 7168 x 2048 15.5 / 12.9.  In 8 bits the same, but for a second wave without adapters (8 rows, 4096 x 9472: 11.2 / 9.6).
+// 17.8 / 13.3 and 7168 x 2048 15.5 / 12.9.  In 8 bits the same, but for a second wave without adapters (8 rows, 4096 x 9472: 11.2 / 9.6), and but for the
+// depth, where the sides cross later (rank 16 / without adapters: 16 rows, 4096 x 4096 9.4 / 13.1 and 6.2 / 7.4, 5120 x 2048 10.9 / 12.4 and 5.4 / 6.6, 8192 x 2048
+// 12.9 / 13.3 and 6.9 / 7.5, 8192 x 1024 12.6 / 12.4 and 6.5 / 6.7; 32 rows, 4096 x 2048 11.2 / 12.4 and 6.2 / 6.5, 8192 x 2048 15.8 / 13.9 and 9.8 / 7.9): one
+// depth for both types, as eight steps in 8 bits would be too deep for 32 rows.
 constexpr int AF_MAX_ROWS = 32;
 inline bool few_rows(int M, int K, int N, int sm_count) {
   return M <= 8 ? N <= 64 * sm_count : M <= AF_MAX_ROWS && K <= 4096 && N <= (M <= 16 ? 64 : 16) * sm_count;
@@ -107,7 +110,7 @@ inline AdaptedTurnPlan plan_adapted_turn(int M, int N, int nkb, int sm_count, in
   return best;
 }
 
-// What the adapters cost the turn kernel beyond what they cost the pair kernel, in us: its products with B grow with the rank and the rows that a block
+// What the adapters cost the turn kernel beyond what they cost the pair kernel, in us (a difference: below zero where the pair kernel loses more by them).  Its products with B grow with the rank and the rows that a block
 // finishes, while the pair kernel has nothing to do when the rank-r product of a deep K comes late (256 rows of 4096 x 4096 in bf16, rank 16 / 64: turn 19.4 / 24.1,
 // pair 24.8 / 27.6; of 1024 x 1024: 10.9 / 14.4 against 10.8 / 12.1; 64 rows of 2048 x 2048 in 8 bits, rank 64: 14.9 / 12.3).
 inline double turn_adapter_cost(int rank, int share, int K) {
@@ -157,7 +160,7 @@ inline ShrinkTcPlan plan_shrink_tc(int M, int nkb, int rank, int n_agents, bool 
   if (M <= 4096) r.tn = std::max(r.tn, std::min(32, (M + 15) / 16 * 16));
   const long long tiles = (M + (long long)r.tn - 1) / r.tn;
   while (r.ks < 8 && tiles * r.ks * 2 <= sm_count && nkb >= r.ks * 4) r.ks *= 2;
-  // Up to 112 rows a block, twice the rows and half the K extent instead: a tile with a second agent then costs half as much more, and A is read half as often
+  // Up to 112 rows a block, twice the rows and half the K extent instead (measured at 4096 deep only): a tile with a second agent then costs half as much more, and A is read half as often
   // (4096 deep, bf16, eight agents' runs of rank 16 / 64, this kernel in us: 3000 rows 18.4 / 21.8 -> 14.1 / 16.6, 4096 19.1 / 22.2 -> 14.4 / 18.0, 8192 20.1 / 24.6 -> 18.8 / 23.4; but
   // 9472 with 128 rows a block 21.0 / 25.4 -> 20.4 / 26.3, 12000 24.5 / 27.5 -> 23.6 / 30.5, and in 8 bits 12000 18.4 / 21.8 -> 19.1 / 27.8).
   const int pair_tn = ((M + sm_count / 2 - 1) / (sm_count / 2) + 15) / 16 * 16;

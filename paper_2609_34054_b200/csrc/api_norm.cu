@@ -7,11 +7,11 @@ using namespace precc;
 namespace {
 
 // Pieces of eight columns per thread (c), threads of a row, and whether several rows share a block.
-// One row or a few: a piece a thread, for latency (1 x 4096: 2.3 us, 2.6 with two, 3.0 with four).  Many rows: what a thread has asked for at once has to cover the
+// One row or a few: a piece a thread, for latency (1 x 4096: 1.7 us, 1.9 with two, 2.3 with four).  Many rows: what a thread has asked for at once has to cover the
 // latency of memory, 64 bytes - two pieces with their residual, or four without.  32768 x 4096, 8-bit output, us with one / two / four pieces: with the
-// residual 187 / 136 / 137, without 180 / 121 / 106 (16384 x 8192 with it: 239 / 144 / 136;
-// 1337 x 3584 without 9.0 / 7.4 / 8.8; eight pieces are slower everywhere).  Many short rows: a warp each, as blocks of one or two
-// warps are bound by how fast blocks start (30000 x 512: 32 us in blocks of 64 threads).
+// residual 189 / 139 / 139, without 157 / 93 / 82 (16384 x 8192: 230 / 141 / 139 and 198 / 104 / 88; both outputs of
+// 1337 x 3584 with it 10.4 / 8.8 / 9.7, without 8.9 / 6.6 / 7.7; eight pieces are slower everywhere).  Many short rows: a warp each, as blocks of one or two
+// warps are bound by how fast blocks start (30000 x 512: 32 us in blocks of 64 threads, 12 with a warp a row).
 struct NormPlan { int c, threads; bool shared_block; };
 NormPlan plan_norm(int rows, int pieces, bool residual) {
   auto whole_warps = [&](int c) { return ((pieces + c - 1) / c + 31) / 32 * 32; };

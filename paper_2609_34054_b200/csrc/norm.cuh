@@ -3,10 +3,10 @@
 //   bf16 output: bf16(y);  8-bit output: scale = max |y| / 448 of the row (1 for a row of zeros), q = e4m3(y / scale)
 //
 // HBM-bound: a row is read once, kept in registers as fp32 from the addition to the last rounding (the norm is of the unrounded
-// sum; every output is rounded once), and written once.  A thread holds C pieces of eight columns, piece i of the row at thread
-// i % T, so that a warp's loads are 512 consecutive bytes.  32768 x 4096 with residual and 8-bit output: 136.7 us, 6.9 TB/s of
-// what is read and written, the rate of a plain copy; both outputs of 1337 x 3584 9.9 us (6.4 from L2).  One row: 1.65 us a call in a graph of
-// such calls.
+// sum; every output is rounded once, the 8-bit one behind a product with 1 / scale), and written once.  A thread holds C pieces of eight columns, piece i of the row
+// at thread i % T, so that a warp's loads are 512 consecutive bytes.  Measured in graphs of calls over rotating inputs: 32768 x 4096 with residual and 8-bit output
+// 136.5 .. 139.8 us, 6.7 .. 6.9 TB/s of what is read and written, the rate of a plain copy; without the residual 83.9 (4.8 TB/s: one block a row, and half the
+// bytes in flight), with both outputs 104 (6.4 TB/s); both outputs of 1337 x 3584 with residual 8.5 us (6.2 from L2).  One row of 2048: 1.4 .. 1.6 us a call.
 #pragma once
 #include "common.cuh"
 

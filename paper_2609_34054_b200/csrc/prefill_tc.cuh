@@ -228,8 +228,6 @@ __device__ __forceinline__ void add2(float& lo, float& hi, float b0, float b1) {
       "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}\n"
       : "+f"(lo), "+f"(hi) : "f"(b0), "f"(b1));
 }
-// True in one lane of the (converged) warp, always the same one.  Unlike a lane-id comparison it tells the compiler that the
-// guarded code runs in a single lane, so MMA and TMA operands stay in uniform registers.
 
 // WL: the work-list form (helper blocks; a block takes a list of tile pieces).  It is a separate instantiation so that
 // the classic launch carries none of its state through the step loop.

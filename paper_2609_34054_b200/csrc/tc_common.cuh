@@ -72,7 +72,8 @@ __device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity,
   return false;
 }
 
-// One lane of a converged warp, the same one every time.
+// True in one lane of the (converged) warp, always the same one.  Unlike a lane-id comparison it tells the compiler that the
+// guarded code runs in a single lane, so MMA and TMA operands stay in uniform registers.
 __device__ __forceinline__ bool elect_one() {
   uint32_t pred;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(pred));
